@@ -431,6 +431,115 @@ fs_status fs_conv_bf16_device_noalloc(const void *d_in, int32_t B, int32_t H, in
                                       int32_t Cout, int32_t kh, int32_t kw, int32_t stride,
                                       int32_t pad, int32_t relu, void *d_out, void *stream);
 
+/* ---- operators on a caller's own device tensors: what comes before and
+ * after an ensemble in a program that has features, heads and logits of its
+ * own.  For all of them:
+ *  - every tensor pointer is a device pointer of the current device (a
+ *    tensor of another device, or host memory, is FS_ERR_INVALID), aligned to
+ *    its elements; rows lie `ld` elements apart (ld >= the row's length, need
+ *    not be a multiple of anything).  Sizes and offsets are 64-bit inside.
+ *  - the call is asynchronous on `stream` (a hipStream_t of the current
+ *    device, NULL = the null stream); it allocates nothing, copies nothing to
+ *    or from the host and may be captured into a graph.
+ *  - only the outputs' elements are written: what lies between or behind the
+ *    rows stays as it was.  Outputs overlap neither inputs nor each other
+ *    unless a call says so.  Results do not depend on scheduling.
+ *  - no rows (M, N or R equal to 0) is a no-op.
+ *  - errors leave a message with fs_last_error(NULL). */
+
+/* What is applied to a product: v, max(0, v), v * Phi(v) (Phi: the normal
+ * distribution function), v / (1 + e^-v).  A NaN stays NaN, except that RELU
+ * gives 0 for it, as it does everywhere in the library. */
+typedef enum { FS_ACT_NONE = 0, FS_ACT_RELU = 1, FS_ACT_GELU = 2, FS_ACT_SILU = 3 } fs_activation;
+
+/* Matrix product with bias, activation and residual:
+ *   s = sum_k x[m][k] * w[n][k] + bias[n]
+ *   y[m][n] = act(s) + res[m][n]      (res_first = 0)
+ *             act(s + res[m][n])      (res_first = 1, the order of a conv)
+ *   d_x    [M][K], d_w [N][K], rows ldx / ldw elements apart
+ *   d_bias [N] fp32, or NULL (= 0)
+ *   d_res  [M][N] in y's type, rows ldres apart (0: one row for all), or NULL
+ *   d_y    [M][N], rows ldy apart; may be d_res with the same row distance
+ * precision is the type of x and w, out_precision that of y and res: FS_F32,
+ * or FS_BF16 for bf16 x and w.  Sums, bias, activation and residual are fp32
+ * and rounded once.  K = 0 is an empty sum.
+ * FS_ERR_INVALID for NULL, negative sizes or rows that are too near;
+ * FS_ERR_UNSUPPORTED for bf16 output of fp32 inputs. */
+fs_status fs_linear_device(const void *d_x, int64_t ldx, const void *d_w, int64_t ldw, const float *d_bias,
+                           const void *d_res, int64_t ldres, void *d_y, int64_t ldy, int32_t M, int32_t N,
+                           int32_t K, int32_t precision, int32_t out_precision, int32_t activation,
+                           int32_t res_first, void *stream);
+
+/* Most alternatives per row, and the bytes of scratch memory of a call below. */
+#define FS_MAX_TOP 128
+#define FS_ROW_SCRATCH_BYTES (2 << 20)
+
+/* Log probabilities of given classes (tokens) under the softmax of each row of
+ * logits, the distribution's entropy, and its most probable classes.
+ *   d_logits  [R][C], FS_F32 or FS_BF16, rows ld apart (fs_infer_device's
+ *             logits are such rows: R = N * B)
+ *   d_classes [R][T] int32: the classes asked for (T may be 0).  One outside
+ *             0..C-1 has probability 0
+ *   K         alternatives per row, 0..FS_MAX_TOP
+ *   d_logp    [R][T] fp32: ln p of the given classes (not read when T = 0)
+ *   d_entropy [R] fp32: -sum p ln p, or NULL
+ *   d_top_ids [R][K] int32, d_top_logp [R][K] fp32: the K most probable classes
+ *             in falling order, equal logits by rising class, and their ln p
+ *             (not read when K = 0)
+ *   d_scratch FS_ROW_SCRATCH_BYTES of device memory, 16-byte aligned, that no
+ *             other call uses until this one has ended on its stream, or NULL: a
+ *             row is then never split over workgroups (slower for few long rows)
+ * A class whose logit is -inf (a mask) has probability 0 and ln p = -inf and is
+ * never an alternative; places without an alternative hold class -1 and -inf.
+ * A row of nothing else has entropy 0.  NaN or +inf in a row makes its ln p and
+ * entropy NaN (-inf where the logit is -inf or the class does not exist);
+ * NaN is never an alternative.
+ * FS_ERR_INVALID for NULL, bad sizes, or when nothing is asked for. */
+fs_status fs_logprob_device(const void *d_logits, int64_t ld, int32_t R, int32_t C, int32_t precision,
+                            const int32_t *d_classes, int32_t T, int32_t K, float *d_logp, float *d_entropy,
+                            int32_t *d_top_ids, float *d_top_logp, void *d_scratch, void *stream);
+
+/* Distillation from a teacher's top classes: the divergence of a student's
+ * distribution p from the teacher's q, and its gradient.  In each row
+ *   q_j = softmax over the row's K entries of top_logp_j / temperature
+ *   p_c = softmax over all C classes of logits_c / temperature
+ *   loss = sum_j q_j (ln q_j - ln p[top_ids_j])
+ *   grad_c = weight / temperature * (p_c - sum of q_j with top_ids_j = c)
+ * (grad = weight * d loss / d logits.)  fs_logprob_device's alternatives are
+ * such a teacher: logits and log probabilities give the same q.
+ *   d_logits   [R][C], FS_F32 or FS_BF16, rows ld apart
+ *   d_top_ids, d_top_logp  [R][K], 1 <= K <= FS_MAX_TOP.  An entry whose class
+ *              lies outside 0..C-1 is left out; a class may come more than
+ *              once; -inf has q = 0
+ *   temperature 1e-6..1e6
+ *   d_weight   [R] fp32, the loss's upstream gradient, or NULL (= 1); read for
+ *              d_grad only
+ *   d_loss     [R] fp32 (without the weight), or NULL
+ *   d_stats    [R][2] fp32: the largest logit m and ln sum_c e^((logits_c - m) /
+ *              temperature), for fs_distill_grad_device, or NULL
+ *   d_grad     [R][C] in the logits' type, rows ldg apart, or NULL; may be
+ *              d_logits with ldg = ld
+ *   d_scratch  as for fs_logprob_device
+ * A row whose teacher has no mass (no entry left, or all -inf) is not trained
+ * on: loss and gradient 0.  A student's -inf (a mask) has p = 0: the loss is
+ * +inf where q > 0.  Statistics of a row of nothing else: -inf and 0.  NaN or
+ * +inf logits give NaN loss and, at classes above -inf, NaN gradients.
+ * FS_ERR_INVALID for NULL, bad sizes or temperature, or when nothing is asked
+ * for. */
+fs_status fs_distill_device(const void *d_logits, int64_t ld, int32_t R, int32_t C, int32_t precision,
+                            const int32_t *d_top_ids, const float *d_top_logp, int32_t K, float temperature,
+                            const float *d_weight, float *d_loss, float *d_stats, void *d_grad, int64_t ldg,
+                            void *d_scratch, void *stream);
+
+/* The gradient alone, from the statistics that fs_distill_device wrote for the
+ * same logits and temperature: one pass over the logits where rows are too long
+ * for one workgroup's registers.  Arguments as above; d_stats and d_grad are
+ * required. */
+fs_status fs_distill_grad_device(const void *d_logits, int64_t ld, int32_t R, int32_t C, int32_t precision,
+                                 const int32_t *d_top_ids, const float *d_top_logp, int32_t K,
+                                 float temperature, const float *d_weight, const float *d_stats,
+                                 void *d_grad, int64_t ldg, void *stream);
+
 /* Number of conv tile configurations fs_test_conv accepts (0..n-1) for a
  * precision, and the name of tile t (NULL when out of range). */
 int32_t fs_conv_num_tiles(int32_t precision);

@@ -176,4 +176,44 @@ constexpr int SOFTMAX_MAX_C = 4096;
 constexpr int COMBINE_MAX_PLURALITY = 64;  // most models FS_COMBINE_PLURALITY takes
 void launch_softmax_combine(const SoftmaxArgs& a, hipStream_t s);
 
+// ------------------------------------------- operators on a caller's tensors
+// Row distances in elements; see the header for the formulas.
+struct LinearArgs {
+  const void* x; int64_t ldx;      // [M][K] storage type
+  const void* w; int64_t ldw;      // [N][K] storage type
+  const float* bias;               // [N] or null
+  const void* res; int64_t ldres;  // [M][N] in y's type, or null
+  void* y; int64_t ldy;            // [M][N]: fp32 if out_f32 else storage type
+  int M, N, K, out_f32, act, res_first;
+};
+void launch_linear(const LinearArgs& a, Prec p, hipStream_t s);
+
+constexpr int MAX_TOP = 128;  // FS_MAX_TOP
+struct LogprobArgs {
+  const void* z; int64_t ld;      // [R][C]
+  const int32_t* classes;         // [R][T]
+  float* logp;                    // [R][T]
+  float* entropy;                 // [R] or null
+  int32_t* top_ids;               // [R][K]
+  float* top_logp;                // [R][K]
+  void* scratch;                  // FS_ROW_SCRATCH_BYTES or null
+  int R, C, T, K;
+};
+void launch_logprob(const LogprobArgs& a, Prec p, hipStream_t s);
+
+struct DistillArgs {
+  const void* z; int64_t ld;      // [R][C]
+  const int32_t* ids;             // [R][K]
+  const float* u;                 // [R][K]
+  const float* weight;            // [R] or null
+  float* loss;                    // [R] or null
+  float* stats;                   // [R][2]: written, or read by the gradient alone
+  void* grad; int64_t ldg;        // [R][C] or null
+  void* scratch;                  // FS_ROW_SCRATCH_BYTES or null
+  float temperature;
+  int R, C, K;
+};
+void launch_distill(const DistillArgs& a, Prec p, hipStream_t s);
+void launch_distill_grad(const DistillArgs& a, Prec p, hipStream_t s);
+
 }  // namespace fs

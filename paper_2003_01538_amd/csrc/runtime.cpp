@@ -22,6 +22,7 @@
 #include <cstdlib>
 #include <cstring>
 #include <functional>
+#include <initializer_list>
 #include <map>
 #include <memory>
 #include <mutex>
@@ -1664,10 +1665,167 @@ int noalloc_tile(ConvArgs& a, int cus) {
   return t;
 }
 
+// ----------------------------------- operators on a caller's device tensors
+// A device pointer of the current device.  The driver's table answers for every
+// allocation on any device and for pinned host memory; pointers that it does
+// not know (ordinary host memory) are refused too.
+void check_on_device(const void* p, int dev, const char* what) {
+  hipPointerAttribute_t at{};
+  if (hipPointerGetAttributes(&at, p) != hipSuccess) {
+    (void)hipGetLastError();
+    fail(FS_ERR_INVALID, std::string(what) + " is not device memory");
+  }
+  if (at.type != hipMemoryTypeDevice && at.type != hipMemoryTypeManaged)
+    fail(FS_ERR_INVALID, std::string(what) + " is not device memory");
+  if (at.type == hipMemoryTypeDevice && at.device != dev)
+    fail(FS_ERR_INVALID, std::string(what) + " is on device " + std::to_string(at.device) + ", the current device is " +
+                             std::to_string(dev));
+}
+
+struct Operand {
+  const void* p;
+  size_t align;
+  const char* what;
+};
+
+// The host side's checks of pointers, before and after the device is known.
+void check_operands(std::initializer_list<Operand> ops, void* stream) {
+  for (const Operand& o : ops)
+    if (o.p && reinterpret_cast<uintptr_t>(o.p) % o.align)
+      fail(FS_ERR_INVALID, std::string(o.what) + " is not aligned to " + std::to_string(o.align) + " bytes");
+  int dev = 0;
+  HIPCHK(hipGetDevice(&dev));
+  if (reinterpret_cast<uintptr_t>(stream) > 2) {  // not one of the runtime's own handles (null, legacy, per thread)
+    hipDevice_t sdev = dev;
+    HIPCHK(hipStreamGetDevice(static_cast<hipStream_t>(stream), &sdev));
+    if (sdev != dev) fail(FS_ERR_INVALID, "the stream is of another device than the current one");
+  }
+  for (const Operand& o : ops)
+    if (o.p) check_on_device(o.p, dev, o.what);
+}
+
+size_t es_of(int32_t precision) { return precision == FS_BF16 ? 2 : 4; }
+
+void check_precision(int32_t precision) {
+  if (precision != FS_F32 && precision != FS_BF16) fail(FS_ERR_INVALID, "precision must be FS_F32 or FS_BF16");
+}
+
+void check_rows(const void* logits, int64_t ld, int32_t R, int32_t C) {
+  if (R < 0 || C < 1) fail(FS_ERR_INVALID, "R must be >= 0 and C >= 1");
+  if (R > 0 && !logits) fail(FS_ERR_INVALID, "logits are required");
+  if (ld < C) fail(FS_ERR_INVALID, "ld must be >= C");
+}
+
+void check_teacher(const DistillArgs& a) {
+  if (a.K < 1 || a.K > FS_MAX_TOP) fail(FS_ERR_INVALID, "K must be in 1..FS_MAX_TOP");
+  if (a.R > 0 && (!a.ids || !a.u)) fail(FS_ERR_INVALID, "top_ids and top_logp are required");
+  if (!(a.temperature >= 1e-6f && a.temperature <= 1e6f)) fail(FS_ERR_INVALID, "temperature must be in 1e-6..1e6");
+  if (a.grad && a.ldg < a.C) fail(FS_ERR_INVALID, "ldg must be >= C");
+  if (a.grad == a.z && a.grad && a.ldg != a.ld) fail(FS_ERR_INVALID, "a gradient over the logits needs ldg = ld");
+}
+
 }  // namespace
 
 // ==================================================================== ABI
 extern "C" {
+
+fs_status fs_linear_device(const void* d_x, int64_t ldx, const void* d_w, int64_t ldw, const float* d_bias,
+                           const void* d_res, int64_t ldres, void* d_y, int64_t ldy, int32_t M, int32_t N, int32_t K,
+                           int32_t precision, int32_t out_precision, int32_t activation, int32_t res_first,
+                           void* stream) {
+  return guarded(nullptr, [&] {
+    check_precision(precision);
+    if (out_precision != FS_F32 && out_precision != FS_BF16) fail(FS_ERR_INVALID, "out_precision must be FS_F32 or FS_BF16");
+    if (precision == FS_F32 && out_precision != FS_F32) fail(FS_ERR_UNSUPPORTED, "fp32 inputs give fp32 output");
+    if (activation < FS_ACT_NONE || activation > FS_ACT_SILU) fail(FS_ERR_INVALID, "unknown activation");
+    if (M < 0 || N < 0 || K < 0) fail(FS_ERR_INVALID, "sizes must be >= 0");
+    if (ldx < K || ldw < K || ldy < N || (d_res && ldres != 0 && ldres < N))
+      fail(FS_ERR_INVALID, "a row distance is shorter than its row");
+    if (M == 0 || N == 0) return;
+    if ((K > 0 && (!d_x || !d_w)) || !d_y) fail(FS_ERR_INVALID, "input, weight and output are required");
+    if (d_res == d_y && ldres != ldy) fail(FS_ERR_INVALID, "an output over the residual needs ldy = ldres");
+    const size_t ei = es_of(precision), eo = es_of(out_precision);
+    check_operands({{K ? d_x : nullptr, ei, "input"}, {K ? d_w : nullptr, ei, "weight"}, {d_bias, 4, "bias"},
+                    {d_res, eo, "residual"}, {d_y, eo, "output"}}, stream);
+    LinearArgs a{};
+    a.x = d_x; a.ldx = ldx; a.w = d_w; a.ldw = ldw; a.bias = d_bias; a.res = d_res; a.ldres = ldres;
+    a.y = d_y; a.ldy = ldy; a.M = M; a.N = N; a.K = K;
+    a.out_f32 = out_precision == FS_F32 ? 1 : 0;
+    a.act = activation; a.res_first = res_first ? 1 : 0;
+    launch_linear(a, precision == FS_BF16 ? BF16 : F32, static_cast<hipStream_t>(stream));
+    HIPCHK(hipGetLastError());
+  });
+}
+
+fs_status fs_logprob_device(const void* d_logits, int64_t ld, int32_t R, int32_t C, int32_t precision,
+                            const int32_t* d_classes, int32_t T, int32_t K, float* d_logp, float* d_entropy,
+                            int32_t* d_top_ids, float* d_top_logp, void* d_scratch, void* stream) {
+  return guarded(nullptr, [&] {
+    check_precision(precision);
+    check_rows(d_logits, ld, R, C);
+    if (T < 0) fail(FS_ERR_INVALID, "T must be >= 0");
+    if (K < 0 || K > FS_MAX_TOP) fail(FS_ERR_INVALID, "K must be in 0..FS_MAX_TOP");
+    if (T == 0 && K == 0 && !d_entropy) fail(FS_ERR_INVALID, "no output is asked for");
+    if (R == 0) return;
+    if (T > 0 && (!d_classes || !d_logp)) fail(FS_ERR_INVALID, "classes and logp are required for T > 0");
+    if (K > 0 && (!d_top_ids || !d_top_logp)) fail(FS_ERR_INVALID, "top_ids and top_logp are required for K > 0");
+    LogprobArgs a{};
+    a.z = d_logits; a.ld = ld;
+    if (T > 0) a.classes = d_classes, a.logp = d_logp;
+    a.entropy = d_entropy;
+    if (K > 0) a.top_ids = d_top_ids, a.top_logp = d_top_logp;
+    a.scratch = d_scratch;
+    a.R = R; a.C = C; a.T = T; a.K = K;
+    check_operands({{a.z, es_of(precision), "logits"}, {a.classes, 4, "classes"}, {a.logp, 4, "logp"},
+                    {a.entropy, 4, "entropy"}, {a.top_ids, 4, "top_ids"}, {a.top_logp, 4, "top_logp"},
+                    {a.scratch, 16, "scratch"}}, stream);
+    launch_logprob(a, precision == FS_BF16 ? BF16 : F32, static_cast<hipStream_t>(stream));
+    HIPCHK(hipGetLastError());
+  });
+}
+
+fs_status fs_distill_device(const void* d_logits, int64_t ld, int32_t R, int32_t C, int32_t precision,
+                            const int32_t* d_top_ids, const float* d_top_logp, int32_t K, float temperature,
+                            const float* d_weight, float* d_loss, float* d_stats, void* d_grad, int64_t ldg,
+                            void* d_scratch, void* stream) {
+  return guarded(nullptr, [&] {
+    check_precision(precision);
+    check_rows(d_logits, ld, R, C);
+    DistillArgs a{};
+    a.z = d_logits; a.ld = ld; a.ids = d_top_ids; a.u = d_top_logp; a.weight = d_grad ? d_weight : nullptr;
+    a.loss = d_loss; a.stats = d_stats; a.grad = d_grad; a.ldg = ldg; a.scratch = d_scratch;
+    a.temperature = temperature; a.R = R; a.C = C; a.K = K;
+    check_teacher(a);
+    if (!d_loss && !d_stats && !d_grad) fail(FS_ERR_INVALID, "no output is asked for");
+    if (R == 0) return;
+    check_operands({{a.z, es_of(precision), "logits"}, {a.ids, 4, "top_ids"}, {a.u, 4, "top_logp"},
+                    {a.weight, 4, "weight"}, {a.loss, 4, "loss"}, {a.stats, 4, "stats"},
+                    {a.grad, es_of(precision), "grad"}, {a.scratch, 16, "scratch"}}, stream);
+    launch_distill(a, precision == FS_BF16 ? BF16 : F32, static_cast<hipStream_t>(stream));
+    HIPCHK(hipGetLastError());
+  });
+}
+
+fs_status fs_distill_grad_device(const void* d_logits, int64_t ld, int32_t R, int32_t C, int32_t precision,
+                                 const int32_t* d_top_ids, const float* d_top_logp, int32_t K, float temperature,
+                                 const float* d_weight, const float* d_stats, void* d_grad, int64_t ldg,
+                                 void* stream) {
+  return guarded(nullptr, [&] {
+    check_precision(precision);
+    check_rows(d_logits, ld, R, C);
+    DistillArgs a{};
+    a.z = d_logits; a.ld = ld; a.ids = d_top_ids; a.u = d_top_logp; a.weight = d_weight;
+    a.stats = const_cast<float*>(d_stats); a.grad = d_grad; a.ldg = ldg;
+    a.temperature = temperature; a.R = R; a.C = C; a.K = K;
+    check_teacher(a);
+    if (R == 0) return;
+    if (!d_stats || !d_grad) fail(FS_ERR_INVALID, "stats and grad are required");
+    check_operands({{a.z, es_of(precision), "logits"}, {a.ids, 4, "top_ids"}, {a.u, 4, "top_logp"},
+                    {a.weight, 4, "weight"}, {a.stats, 4, "stats"}, {a.grad, es_of(precision), "grad"}}, stream);
+    launch_distill_grad(a, precision == FS_BF16 ? BF16 : F32, static_cast<hipStream_t>(stream));
+    HIPCHK(hipGetLastError());
+  });
+}
 
 fs_status fs_conv_bf16_device_noalloc(const void* d_in, int32_t B, int32_t H, int32_t W, int32_t Cin, const void* d_w,
                                       const float* d_bias, const void* d_res, int32_t Cout, int32_t kh, int32_t kw,

@@ -24,6 +24,9 @@ FS_OK, FS_ERR_INVALID, FS_ERR_OOM, FS_ERR_DEVICE, FS_ERR_UNSUPPORTED, FS_ERR_INT
 FS_F32, FS_BF16 = 0, 1
 FS_OP_CONV, FS_OP_MAXPOOL, FS_OP_GAP, FS_OP_FC = range(4)
 FS_COMBINE_MEAN, FS_COMBINE_PLURALITY, FS_COMBINE_ANY = range(3)
+FS_ACT_NONE, FS_ACT_RELU, FS_ACT_GELU, FS_ACT_SILU = range(4)
+FS_MAX_TOP = 128
+FS_ROW_SCRATCH_BYTES = 2 << 20
 STATUS_NAMES = {0: "FS_OK", 1: "FS_ERR_INVALID", 2: "FS_ERR_OOM", 3: "FS_ERR_DEVICE",
                 4: "FS_ERR_UNSUPPORTED", 5: "FS_ERR_INTERNAL"}
 
@@ -144,6 +147,15 @@ SIGNATURES = [
     ("fs_conv_bf16_device_noalloc", ctypes.c_int, [_vp, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
                                                    ctypes.c_int32, _vp, _fp, _vp] + [ctypes.c_int32] * 6 +
                                                   [_vp, _vp]),
+    ("fs_linear_device", ctypes.c_int, [_vp, ctypes.c_int64, _vp, ctypes.c_int64, _vp, _vp, ctypes.c_int64, _vp,
+                                        ctypes.c_int64] + [ctypes.c_int32] * 7 + [_vp]),
+    ("fs_logprob_device", ctypes.c_int, [_vp, ctypes.c_int64] + [ctypes.c_int32] * 3 + [_vp] + [ctypes.c_int32] * 2 +
+                                        [_vp] * 6),
+    ("fs_distill_device", ctypes.c_int, [_vp, ctypes.c_int64] + [ctypes.c_int32] * 3 + [_vp, _vp, ctypes.c_int32,
+                                        ctypes.c_float, _vp, _vp, _vp, _vp, ctypes.c_int64, _vp, _vp]),
+    ("fs_distill_grad_device", ctypes.c_int, [_vp, ctypes.c_int64] + [ctypes.c_int32] * 3 +
+                                             [_vp, _vp, ctypes.c_int32, ctypes.c_float, _vp, _vp, _vp, ctypes.c_int64,
+                                              _vp]),
     ("fs_conv_num_tiles", ctypes.c_int32, [ctypes.c_int32]),
     ("fs_conv_tile_name", ctypes.c_char_p, [ctypes.c_int32, ctypes.c_int32]),
 ]
@@ -541,6 +553,38 @@ def fs_bench_conv(B, H, W, Cin, Cout, k, stride, pad, relu=1, residual=0, precis
     _check(load().fs_bench_conv(B, H, W, Cin, Cout, k, k, stride, pad, relu, residual, precision, tile, Z,
                                 iters, ctypes.byref(ms), ctypes.byref(used), device))
     return ms.value, used.value
+
+
+# Operators on a caller's device tensors.  Every pointer is an integer device
+# address (e.g. torch data_ptr()), 0 for an optional tensor that is not there.
+def fs_linear_device(d_x, ldx, d_w, ldw, d_bias, d_res, ldres, d_y, ldy, M, N, K, precision, out_precision,
+                     activation=FS_ACT_NONE, res_first=0, stream=0):
+    """y = act(x . w^T + bias) + res, or act(x . w^T + bias + res)."""
+    _check(load().fs_linear_device(d_x, ldx, d_w, ldw, d_bias or None, d_res or None, ldres, d_y, ldy, M, N, K,
+                                   precision, out_precision, activation, res_first, stream or None))
+
+
+def fs_logprob_device(d_logits, ld, R, C, precision, d_classes, T, K, d_logp, d_entropy, d_top_ids, d_top_logp,
+                      d_scratch=0, stream=0):
+    """ln p of given classes, entropy and the K most probable classes of each row of logits."""
+    _check(load().fs_logprob_device(d_logits, ld, R, C, precision, d_classes or None, T, K, d_logp or None,
+                                    d_entropy or None, d_top_ids or None, d_top_logp or None, d_scratch or None,
+                                    stream or None))
+
+
+def fs_distill_device(d_logits, ld, R, C, precision, d_top_ids, d_top_logp, K, temperature, d_weight, d_loss, d_stats,
+                      d_grad, ldg, d_scratch=0, stream=0):
+    """Divergence of each row's softmax from a teacher's top classes, and its gradient."""
+    _check(load().fs_distill_device(d_logits, ld, R, C, precision, d_top_ids, d_top_logp, K, temperature,
+                                    d_weight or None, d_loss or None, d_stats or None, d_grad or None, ldg,
+                                    d_scratch or None, stream or None))
+
+
+def fs_distill_grad_device(d_logits, ld, R, C, precision, d_top_ids, d_top_logp, K, temperature, d_weight, d_stats,
+                           d_grad, ldg, stream=0):
+    """The gradient alone, from fs_distill_device's statistics."""
+    _check(load().fs_distill_grad_device(d_logits, ld, R, C, precision, d_top_ids, d_top_logp, K, temperature,
+                                         d_weight or None, d_stats, d_grad, ldg, stream or None))
 
 
 def fs_conv_num_tiles(precision) -> int:

@@ -1,0 +1,131 @@
+"""Refusals of the operators on a caller's tensors (no GPU: every check of
+sizes, types and NULLs comes before any device call), and the definitions in
+64 bits against properties and differences."""
+import ctypes
+
+import numpy as np
+import pytest
+
+from oracle import operators as ref
+from paper_2003_01538_amd import flexserve as fsb
+
+P = 4096  # an address that no check of arguments reads
+BF, F = fsb.FS_BF16, fsb.FS_F32
+LIN = dict(x=P, ldx=8, w=P, ldw=8, bias=0, res=0, ldres=0, y=P, ldy=4, M=2, N=4, K=8, prec=BF, out=F, act=0, first=0,
+           stream=0)
+LGP = dict(z=P, ld=10, R=2, C=10, prec=F, classes=P, T=1, K=3, logp=P, entropy=0, ids=P, best=P, scratch=0, stream=0)
+DST = dict(z=P, ld=10, R=2, C=10, prec=F, ids=P, u=P, K=3, tau=1.0, weight=0, loss=P, stats=0, grad=0, ldg=10, scratch=0,
+           stream=0)
+GRD = dict(z=P, ld=10, R=2, C=10, prec=F, ids=P, u=P, K=3, tau=1.0, weight=0, stats=P, grad=P, ldg=10, stream=0)
+INV, UNS = fsb.FS_ERR_INVALID, fsb.FS_ERR_UNSUPPORTED
+
+
+def status(fn, base, **change):
+    try:
+        fn(*{**base, **change}.values())
+    except fsb.FsError as e:
+        assert fsb.fs_last_error()
+        return e.status
+    return fsb.FS_OK
+
+
+@pytest.mark.parametrize("change,want", [
+    (dict(x=None), INV), (dict(w=None), INV), (dict(y=None), INV), (dict(M=-1), INV), (dict(N=-1), INV),
+    (dict(K=-1), INV), (dict(ldx=7), INV), (dict(ldw=7), INV), (dict(ldy=3), INV), (dict(res=P, ldres=3), INV),
+    (dict(res=P, ldres=-4), INV), (dict(prec=2), INV), (dict(out=2), INV), (dict(act=4), INV), (dict(act=-1), INV),
+    (dict(prec=F, out=BF), UNS), (dict(x=P + 1), INV), (dict(bias=P + 2), INV), (dict(y=P + 2), INV),
+    (dict(res=P, ldres=5), INV),  # over the output with another row distance
+    (dict(M=0, x=None), fsb.FS_OK), (dict(N=0, ldy=0, w=None), fsb.FS_OK),
+])
+def test_linear_refuses(change, want):
+    assert status(fsb.fs_linear_device, LIN, **change) == want
+
+
+@pytest.mark.parametrize("change,want", [
+    (dict(z=None), INV), (dict(R=-1), INV), (dict(C=0), INV), (dict(ld=9), INV), (dict(prec=3), INV), (dict(T=-1), INV),
+    (dict(K=-1), INV), (dict(K=129), INV), (dict(classes=0), INV), (dict(logp=0), INV), (dict(ids=0), INV),
+    (dict(best=0), INV), (dict(T=0, K=0), INV), (dict(z=P + 2), INV), (dict(scratch=P + 8), INV), (dict(entropy=P + 2), INV),
+    (dict(R=0, z=None), fsb.FS_OK),
+])
+def test_logprob_refuses(change, want):
+    assert status(fsb.fs_logprob_device, LGP, **change) == want
+
+
+@pytest.mark.parametrize("fn,base", [(fsb.fs_distill_device, DST), (fsb.fs_distill_grad_device, GRD)])
+@pytest.mark.parametrize("change,want", [
+    (dict(z=None), INV), (dict(R=-1), INV), (dict(C=0), INV), (dict(ld=9), INV), (dict(prec=3), INV), (dict(K=0), INV),
+    (dict(K=129), INV), (dict(ids=None), INV), (dict(u=None), INV), (dict(tau=0.0), INV), (dict(tau=-1.0), INV),
+    (dict(tau=float("nan")), INV), (dict(tau=float("inf")), INV), (dict(tau=1e-7), INV), (dict(grad=P, ldg=9), INV),
+    (dict(grad=P, ld=11), INV), (dict(u=P + 2), INV), (dict(weight=P + 1, grad=P + 64), INV),
+    (dict(R=0, z=None, ids=None, u=None), fsb.FS_OK),
+])
+def test_distill_refuses(fn, base, change, want):
+    assert status(fn, base, **change) == want
+
+
+def test_distill_wants_an_output():
+    assert status(fsb.fs_distill_device, DST, loss=0) == INV
+    assert status(fsb.fs_distill_grad_device, GRD, stats=0) == INV
+    assert status(fsb.fs_distill_grad_device, GRD, grad=0) == INV
+
+
+def test_valid_call_without_a_device_reports_it():
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("a device is present")
+    host = (ctypes.c_float * 64)()
+    a = ctypes.addressof(host)
+    a += -a % 16
+    for fn, base in ((fsb.fs_linear_device, dict(LIN, x=a, w=a, y=a)),
+                     (fsb.fs_logprob_device, dict(LGP, z=a, classes=a, logp=a, ids=a, best=a)),
+                     (fsb.fs_distill_device, dict(DST, z=a, ids=a, u=a, loss=a)),
+                     (fsb.fs_distill_grad_device, dict(GRD, z=a, ids=a, u=a, stats=a, grad=a))):
+        assert status(fn, base) == fsb.FS_ERR_DEVICE
+
+
+def test_constants_agree_with_the_header():
+    import os
+    import re
+    h = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "flexserve.h")).read()
+    assert int(re.search(r"#define FS_MAX_TOP (\d+)", h).group(1)) == fsb.FS_MAX_TOP
+    a, b = re.search(r"#define FS_ROW_SCRATCH_BYTES \((\d+) << (\d+)\)", h).groups()
+    assert int(a) << int(b) == fsb.FS_ROW_SCRATCH_BYTES
+
+
+# ------------------------------------------------- the definitions themselves
+def test_gradient_definition_against_differences():
+    rng = np.random.default_rng(5)
+    z = rng.standard_normal((3, 9)) * 3
+    ids = np.array([[1, 4, 1], [8, -1, 0], [2, 3, 9]])  # a class twice, entries that are left out
+    u = rng.standard_normal((3, 3))
+    w = np.array([0.5, 2.0, 1.5])
+    for tau in (0.5, 1.0, 4.0):
+        g = ref.distill(z, ids, u, tau, w)["grad"]
+        for r in range(3):
+            for c in range(9):
+                up, dn = z.copy(), z.copy()
+                up[r, c] += 1e-5
+                dn[r, c] -= 1e-5
+                d = (ref.distill(up, ids, u, tau)["loss"][r] - ref.distill(dn, ids, u, tau)["loss"][r]) / 2e-5
+                # the difference's own error: third derivatives of order 1 / tau^3 times 1e-10, and 1e-16 / 1e-5 of rounding
+                assert abs(g[r, c] - w[r] * d) < 1e-8, (tau, r, c)
+
+
+def test_definitions_of_the_edges():
+    inf, nan = np.inf, np.nan
+    z = np.array([[0.0, 0.0, -inf, 0.0], [-inf] * 4, [1.0, nan, 2.0, -inf], [3.0, inf, 0.0, 1.0]])
+    o = ref.logprob(z, np.array([[0, 2], [0, -1], [0, 3], [1, 4]]), 5)
+    assert np.allclose(o["logp"][0, 0], -np.log(3)) and o["logp"][0, 1] == -inf
+    assert (o["logp"][1] == -inf).all() and o["entropy"][1] == 0 and np.allclose(o["entropy"][0], np.log(3))
+    assert np.isnan(o["logp"][2, 0]) and o["logp"][2, 1] == -inf and np.isnan(o["entropy"][2])
+    assert o["top_ids"].tolist() == [[0, 1, 3, -1, -1], [-1] * 5, [2, 0, -1, -1, -1], [1, 0, 3, 2, -1]]
+    d = ref.distill(z, np.array([[0, -1], [0, 1], [0, 2], [4, 7]]), np.zeros((4, 2)), 1.0)
+    assert np.allclose(d["loss"][0], np.log(3)) and d["loss"][1] == inf and np.isnan(d["loss"][2]) and d["loss"][3] == 0
+    assert np.allclose(d["grad"][1], [-0.5, -0.5, 0, 0]) and (d["grad"][3] == 0).all() and d["grad"][2, 3] == 0
+
+
+def test_activations_against_known_values():
+    v = np.array([-1.0, 0.0, 1.0, 30.0])
+    assert np.allclose(ref.activation(v, 2), [-0.15865525393145707, 0, 0.8413447460685429, 30])
+    assert np.allclose(ref.activation(v, 3), [-0.2689414213699951, 0, 0.7310585786300049, 30])
+    assert ref.activation(np.array([-800.0]), 3)[0] == 0
