@@ -5,9 +5,22 @@
 // One workgroup per row.
 #include "rows.hpp"
 
+
 namespace fs {
 
 namespace {
+
+constexpr int ROW_T = 256;
+
+template <class T>
+__device__ void row_stats(const T* z, int C, float c, float* sh, float& m, float& s, float& t) {
+  float best = -FLT_MAX;
+  for (int i = threadIdx.x; i < C; i += ROW_T) best = fmaxf(best, RowT<T>::one(z + i));
+  m = block_max<ROW_T>(best, sh);
+  s = t = 0.f;
+  for (int i = threadIdx.x; i < C; i += ROW_T) s += expf((RowT<T>::one(z + i) - m) * c);
+  s = block_sum<ROW_T>(s, sh);
+}
 
 // The row's teacher in LDS: q[j] (0 for an entry that is left out) and id[j]
 // (-1 for one).  Returns whether the teacher has any mass.
@@ -21,9 +34,9 @@ __device__ bool teacher(const DistillArgs& a, int64_t row, float c, float* q, in
     else u = a.u[row * a.K + j];
   }
   const bool mass = __syncthreads_or(!(u == -INFINITY));
-  const float m = block_max(fmaxf(u, -FLT_MAX), sh);
+  const float m = block_max<ROW_T>(fmaxf(u, -FLT_MAX), sh);
   const float e = k < 0 ? 0.f : expf((u - m) * c);
-  const float s = block_sum(e, sh);
+  const float s = block_sum<ROW_T>(e, sh);
   if (j < a.K) { q[j] = mass ? e / s : 0.f; id[j] = k; }
   __syncthreads();
   return mass;
@@ -53,13 +66,13 @@ __global__ void __launch_bounds__(ROW_T) k_distill(DistillArgs a) {
     const int cj = j < a.K ? id[j] : -1;
     float lp = 0.f;
     if (cj >= 0) {
-      const float x = row_load(z + cj);
+      const float x = RowT<T>::one(z + cj);
       lp = x == -INFINITY ? -INFINITY : (x - m) * c - l;
     }
     if (STATS && a.loss) {
       float part = 0.f;
       if (cj >= 0 && q[j] != 0.f) part = q[j] * (logf(q[j]) - lp);
-      const float loss = block_sum(part, sh);
+      const float loss = block_sum<ROW_T>(part, sh);
       if (threadIdx.x == 0) a.loss[row] = mass ? loss : 0.f;
     }
     if (a.grad) {
@@ -67,14 +80,14 @@ __global__ void __launch_bounds__(ROW_T) k_distill(DistillArgs a) {
       const float wt = (a.weight ? a.weight[row] : 1.f) * c;
       __syncthreads();
       for (int i = threadIdx.x; i < a.C; i += ROW_T) {
-        const float x = row_load(z + i);
-        row_store(g + i, !mass ? 0.f : x == -INFINITY ? 0.f : expf((x - m) * c - l) * wt);
+        const float x = RowT<T>::one(z + i);
+        RowT<T>::put(g + i, !mass ? 0.f : x == -INFINITY ? 0.f : expf((x - m) * c - l) * wt);
       }
       __syncthreads();
       if (mass && cj >= 0) {
         float sum = 0.f;  // entries of one class write the same value
         for (int i = 0; i < a.K; ++i) sum += id[i] == cj ? q[i] : 0.f;
-        row_store(g + cj, (expf(lp) - sum) * wt);
+        RowT<T>::put(g + cj, (expf(lp) - sum) * wt);
       }
     }
     __syncthreads();

@@ -1,10 +1,11 @@
-// Softmax statistics of a row of logits, for the operators that read rows of
-// any length (log probabilities, distillation).
+// Rows of logits of any length and alignment, and their softmax statistics,
+// for the operators that read such rows (log probabilities, distillation).
 //
 // m is the largest logit, at least the lowest finite number: a row of nothing
-// but -inf then sums to 0 instead of NaN, and a finite lowest value (some
-// masks) still counts.  s = sum e^((z - m) c) and t = sum e^((z - m) c) (z - m) are kept
-// in fp32, c = 1 / temperature.
+// but -inf then sums to 0 instead of NaN, and a finite lowest value (some masks)
+// still counts.  s = sum e^((z - m) c) and t = sum e^((z - m) c) (z - m) are kept
+// in fp32, c = 1 / temperature.  z - m is formed before the scaling, so the error
+// of an exponential follows its distance from the maximum, not the logit's size.
 #pragma once
 
 #include <float.h>
@@ -15,12 +16,66 @@
 
 namespace fs {
 
-constexpr int ROW_T = 256;  // threads of a workgroup
+constexpr float LOG2E = 1.44269504f;
+constexpr float FAR = -200.f;  // e^FAR is 0 in fp32: a bound for z - m where it is multiplied by such an exponential
 
-__device__ __forceinline__ float row_load(const float* p) { return *p; }
-__device__ __forceinline__ float row_load(const uint16_t* p) { return bf2f(*p); }
-__device__ __forceinline__ void row_store(float* p, float v) { *p = v; }
-__device__ __forceinline__ void row_store(uint16_t* p, float v) { *p = f2bf(v); }
+// 16 bytes of a row at any element: the hardware takes vector accesses at
+// every byte address.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 u32x4_at2 __attribute__((aligned(2)));
+typedef u32x4 u32x4_at4 __attribute__((aligned(4)));
+
+template <class T> struct RowT;
+template <> struct RowT<float> {
+  static constexpr int VEC = 4;
+  static __device__ __forceinline__ u32x4 load(const float* p) { return *reinterpret_cast<const u32x4_at4*>(p); }
+  static __device__ __forceinline__ void store(float* p, u32x4 v) { *reinterpret_cast<u32x4_at4*>(p) = v; }
+  static __device__ __forceinline__ float get(u32x4 v, int e) { return __uint_as_float(v[e]); }
+  static __device__ __forceinline__ float one(const float* p) { return *p; }
+  static __device__ __forceinline__ void put(float* p, float v) { *p = v; }
+  static __device__ __forceinline__ u32x4 pack(const float* f) {
+    return u32x4{__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3])};
+  }
+};
+template <> struct RowT<uint16_t> {  // bf16
+  static constexpr int VEC = 8;
+  static __device__ __forceinline__ u32x4 load(const uint16_t* p) { return *reinterpret_cast<const u32x4_at2*>(p); }
+  static __device__ __forceinline__ void store(uint16_t* p, u32x4 v) { *reinterpret_cast<u32x4_at2*>(p) = v; }
+  static __device__ __forceinline__ float get(u32x4 v, int e) {
+    return __uint_as_float(e & 1 ? v[e >> 1] & 0xffff0000u : v[e >> 1] << 16);
+  }
+  static __device__ __forceinline__ float one(const uint16_t* p) { return bf2f(*p); }
+  static __device__ __forceinline__ void put(uint16_t* p, float v) { *p = f2bf(v); }
+  static __device__ __forceinline__ u32x4 pack(const float* f) {
+    const uint4 u = f8_to_bf8(f);
+    return u32x4{u.x, u.y, u.z, u.w};
+  }
+};
+
+// Elements i .. i + VEC - 1 of a row that ends at `end`; -inf behind the end.
+template <class T>
+__device__ __forceinline__ u32x4 row_vec(const T* z, int64_t i, int64_t end) {
+  constexpr int VEC = RowT<T>::VEC;
+  if (i + VEC <= end) return RowT<T>::load(z + i);
+  float f[VEC];
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) f[e] = i + e < end ? RowT<T>::one(z + i + e) : -INFINITY;
+  return RowT<T>::pack(f);
+}
+
+// NV vectors of a workgroup's chunk of NT * NV vectors that begins at `from`:
+// thread t holds vectors t, t + NT, ...
+template <class T, int NT, int NV>
+__device__ __forceinline__ void row_chunk(const T* z, int64_t from, int64_t end, u32x4 (&v)[NV]) {
+  constexpr int VEC = RowT<T>::VEC;
+  if (from + NT * NV * VEC <= end) {  // the same for the whole workgroup
+#pragma unroll
+    for (int j = 0; j < NV; ++j) v[j] = RowT<T>::load(z + from + (j * NT + (int)threadIdx.x) * VEC);
+  } else {
+#pragma unroll
+    for (int j = 0; j < NV; ++j) v[j] = row_vec(z, from + (j * NT + (int)threadIdx.x) * VEC, end);
+  }
+}
 
 __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
@@ -28,41 +83,58 @@ __device__ __forceinline__ float wave_max(float v) {
   return v;
 }
 
-// Sum or maximum over the workgroup, the same in every thread; `sh` holds one
-// value per wave and is free again after the call.
+// Sum or maximum over a workgroup of NT threads, the same in every thread; `sh`
+// holds one value per wave and is free again after the call.
+template <int NT>
 __device__ __forceinline__ float block_sum(float v, float* sh) {
   v = wave_sum(v);
-  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = 0.f;
-  for (int w = 0; w < ROW_T / 64; ++w) v += sh[w];
-  __syncthreads();
+  if constexpr (NT > 64) {
+    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.f;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) v += sh[w];
+    __syncthreads();
+  }
   return v;
 }
+template <int NT>
 __device__ __forceinline__ float block_max(float v, float* sh) {
   v = wave_max(v);
-  if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = sh[0];
-  for (int w = 1; w < ROW_T / 64; ++w) v = fmaxf(v, sh[w]);
-  __syncthreads();
+  if constexpr (NT > 64) {
+    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = sh[0];
+#pragma unroll
+    for (int w = 1; w < NT / 64; ++w) v = fmaxf(v, sh[w]);
+    __syncthreads();
+  }
   return v;
 }
 
-// m, s, t of a row, in every thread
-template <class T>
-__device__ void row_stats(const T* z, int C, float c, float* sh, float& m, float& s, float& t) {
-  float best = -FLT_MAX;
-  for (int i = threadIdx.x; i < C; i += ROW_T) best = fmaxf(best, row_load(z + i));
-  m = block_max(best, sh);
-  s = t = 0.f;
-  for (int i = threadIdx.x; i < C; i += ROW_T) {
-    const float d = row_load(z + i) - m, e = expf(d * c);
-    s += e;
-    t += e > 0.f ? e * d : 0.f;
+// Running statistics of the logits that a thread has seen.  k2 = log2(e) c.
+// T: whether t is wanted (c is 1 then).
+template <bool T>
+struct RowStats {
+  float m = -FLT_MAX, s = 0.f, t = 0.f;
+  // raise the maximum to mn
+  __device__ __forceinline__ void lift(float mn, float k2) {
+    const float d = m - mn, f = __builtin_amdgcn_exp2f(d * k2);
+    if constexpr (T) t = f * (t + fmaxf(d, FAR) * s);
+    s *= f;
+    m = mn;
   }
-  s = block_sum(s, sh);
-  t = block_sum(t, sh);
-}
+  __device__ __forceinline__ void add(float z, float k2) {
+    const float d = z - m, e = __builtin_amdgcn_exp2f(d * k2);
+    s += e;
+    if constexpr (T) t = fmaf(e, fmaxf(d, FAR), t);
+  }
+  template <int NT>
+  __device__ __forceinline__ void over_block(float k2, float* sh) {
+    lift(block_max<NT>(m, sh), k2);
+    s = block_sum<NT>(s, sh);
+    if constexpr (T) t = block_sum<NT>(t, sh);
+  }
+};
 
 }  // namespace fs
