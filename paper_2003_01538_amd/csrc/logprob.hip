@@ -36,10 +36,8 @@ __device__ __forceinline__ uint32_t order_key(float z) {
   return b ^ (uint32_t(int32_t(b) >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ uint64_t entry(float z, int c) { return uint64_t(order_key(z)) << 32 | ~uint32_t(c); }
-__device__ __forceinline__ float entry_logit(uint64_t e) {
-  const uint32_t k = uint32_t(e >> 32);
-  return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k);
-}
+__device__ __forceinline__ float key_logit(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
+__device__ __forceinline__ float entry_logit(uint64_t e) { return key_logit(uint32_t(e >> 32)); }
 __device__ __forceinline__ int entry_class(uint64_t e) { return int(~uint32_t(e)); }
 
 constexpr int SLACK = 64;  // entries that the list grows by before it is cut
@@ -47,10 +45,20 @@ constexpr int SLACK = 64;  // entries that the list grows by before it is cut
 template <int NT>
 struct Selection {
   static constexpr int LIST = NT == 64 ? 512 : 1024;
-  uint64_t list[LIST];
+  __attribute__((aligned(16))) uint64_t list[LIST];
   uint64_t top[MAX_TOP];
-  uint32_t maxima[NT];
+  float maxima[NT];
   int hits[3], n, count[NT / 64];
+};
+
+// What a workgroup knows of its selection, the same in every thread: the K-th
+// best logit so far (-inf: fewer than K), the list's length, whether the list is
+// cut (at most K entries in falling order), and the number of chunks seen.
+struct Progress {
+  float bar = -INFINITY;
+  int n = 0;
+  bool sorted = true;
+  int turn = 0;
 };
 
 // Sum over the workgroup of a number that is already the wave's.
@@ -67,114 +75,156 @@ __device__ __forceinline__ int block_count(int v, int* sh) {
   return v;
 }
 
-// Cut the list's n entries to the K best, in falling order; returns how many remain.
+// Cut the list to the K best, in falling order.
 template <int NT>
-__device__ int cut(Selection<NT>& S, int n, int K) {
+__device__ __forceinline__ void cut(Selection<NT>& S, Progress& p, int K) {
+  if (p.sorted) return;
+  const int n = p.n;
   for (int i = threadIdx.x; i < n; i += NT) {
     const uint64_t own = S.list[i];
-    int rank = 0;
-    for (int j = 0; j < n; ++j) rank += S.list[j] > own ? 1 : 0;
+    int rank = 0, j = 0;
+    for (; j + 8 <= n; j += 8)
+#pragma unroll
+      for (int u = 0; u < 8; ++u) rank += S.list[j + u] > own ? 1 : 0;
+    for (; j < n; ++j) rank += S.list[j] > own ? 1 : 0;
     if (rank < K) S.top[rank] = own;
   }
   __syncthreads();
-  n = min(n, K);
-  for (int i = threadIdx.x; i < n; i += NT) S.list[i] = S.top[i];
-  if (threadIdx.x == 0) S.n = n;
+  p.n = min(n, K);
+  for (int i = threadIdx.x; i < p.n; i += NT) S.list[i] = S.top[i];
+  if (threadIdx.x == 0) S.n = p.n;
+  p.sorted = true;
   __syncthreads();
-  return n;
+}
+
+// The largest number of which count() says at least K, searched from the highest
+// bit down; ends early once count() says at most `most`.
+template <class Count>
+__device__ __forceinline__ uint32_t search(int K, int most, Count&& count) {
+  uint32_t x = 0;
+  for (int bit = 31; bit >= 0; --bit) {
+    const int c = count(x | 1u << bit);
+    if (c < K) continue;
+    x |= 1u << bit;
+    if (c <= most) break;
+  }
+  return x;
 }
 
 // One chunk's candidates into the list.  get(j, z, c): this thread's j-th of NE
-// logits and its class; best: the largest of them (-inf: none).  `bar` is the
-// K-th best logit so far (-inf: fewer than K), n the list's length, `turn` counts the
-// calls; the three are the same in every thread.
+// logits and its class; best: the largest of them (-inf: none).
 template <int NT, int NE, class Get>
-__device__ __forceinline__ void select_chunk(Selection<NT>& S, int K, float best, Get&& get, float& bar, int& n, int turn) {
+__device__ __forceinline__ void select_chunk(Selection<NT>& S, Progress& p, int K, float best, Get&& get) {
   constexpr int LIST = Selection<NT>::LIST;
-  const int lane = threadIdx.x & 63;
-  const uint64_t wave_hits = __ballot(best > bar);
+  const int lane = threadIdx.x & 63, turn = p.turn++;
+  const uint64_t wave_hits = __ballot(best > p.bar);
   int hits;
   if constexpr (NT == 64) {
-    hits = __popcll(wave_hits);
+    hits = (int)__popcll(wave_hits);
   } else {
     // three counters in turn: the one of two calls on is cleared while no wave can be there yet
     if (wave_hits && lane == 0) atomicAdd(&S.hits[turn % 3], (int)__popcll(wave_hits));
+    if (turn == 0) S.maxima[threadIdx.x] = best;
     __syncthreads();
     hits = S.hits[turn % 3];
     if (threadIdx.x == 0) S.hits[(turn + 2) % 3] = 0;
   }
   if (hits == 0) return;
 
-  uint64_t least = 0;  // entries below this are not listed
-  const bool many = n + hits * NE > LIST;
+  // candidates: z >= from, the logit next above the bar
+  float from = key_logit(order_key(p.bar) + 1);
+  const bool many = p.n + hits * NE > LIST;
   if (many) {
-    if (n > K) n = cut(S, n, K);
-    const int most = LIST - n;
-    // over the threads' maxima: the key that K or a few more of them reach
-    uint32_t key = 0;
+    cut(S, p, K);
+    // a logit that K or a few more of the threads' maxima reach, of groups of threads if those are enough
     if (hits > K) {
-      S.maxima[threadIdx.x] = best > bar ? order_key(best) : 0;
-      __syncthreads();
-      uint32_t mx[NT / 64];
+      if constexpr (NT == 64) {
+        from = fmaxf(from, key_logit(search(K, K + (K >> 3) + 2, [&](uint32_t k) { return (int)__popcll(__ballot(best >= key_logit(k))); })));
+      } else {
+        if (turn > 0) {
+          S.maxima[threadIdx.x] = best;
+          __syncthreads();
+        }
+        float q[NT / 64], g = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < NT / 64; ++w) mx[w] = S.maxima[w * 64 + lane];
-      for (int bit = 31; bit >= 0; --bit) {
-        const uint32_t up = key | 1u << bit;
-        int c = 0;
+        for (int w = 0; w < NT / 64; ++w) {
+          q[w] = S.maxima[w * 64 + lane];
+          g = fmaxf(g, q[w]);
+        }
+        uint32_t k;
+        if (K <= 40 && (int)__popcll(__ballot(g >= from)) >= K)
+          k = search(K, K + (K >> 3) + 2, [&](uint32_t k) { return (int)__popcll(__ballot(g >= key_logit(k))); });
+        else
+          k = search(K, K + (K >> 3) + 2, [&](uint32_t k) {
+            int c = 0;
 #pragma unroll
-        for (int w = 0; w < NT / 64; ++w) c += (int)__popcll(__ballot(mx[w] >= up));
-        if (c < K) continue;
-        key = up;
-        if (c <= K + (K >> 3) + 2) break;
-      }
-    }
-    least = uint64_t(key) << 32;
-    // too many logits of the chunk there: over the chunk, down to the class
-    auto reach = [&](uint64_t lo) {
-      int c = 0;
-#pragma unroll
-      for (int j = 0; j < NE; ++j) {
-        float z;
-        int k;
-        get(j, z, k);
-        c += (int)__popcll(__ballot(z > bar && entry(z, k) >= lo));
-      }
-      return block_count<NT>(c, S.count);
-    };
-    if (reach(least) > most) {
-      least = 0;
-      for (int bit = 63; bit >= 0; --bit) {
-        const uint64_t up = least | 1ull << bit;
-        const int c = reach(up);
-        if (c < K) continue;
-        least = up;
-        if (c <= most) break;
+            for (int w = 0; w < NT / 64; ++w) c += (int)__popcll(__ballot(q[w] >= key_logit(k)));
+            return c;
+          });
+        from = fmaxf(from, key_logit(k));
       }
     }
   }
-  if (wave_hits) {
+  // list them, all of a wave's in one place; false: there is no room for them
+  auto list = [&](auto&& takes) {
+    uint32_t mine = 0;  // bit j: this thread's j-th logit
 #pragma unroll
     for (int j = 0; j < NE; ++j) {
       float z;
-      int k;
-      get(j, z, k);
-      const uint64_t e = entry(z, k);
-      const bool take = z > bar && e >= least;
-      const uint64_t b = __ballot(take);
-      if (!b) continue;
-      int at = 0;
-      if (lane == 0) at = atomicAdd(&S.n, (int)__popcll(b));
-      at = __builtin_amdgcn_readfirstlane(at);
-      if (take) S.list[at + __popcll(b & ((1ull << lane) - 1))] = e;
+      int c;
+      get(j, z, c);
+      mine |= (takes(z, c) ? 1u : 0u) << j;
     }
-  }
+    const int count = __popc(mine), upto = wave_scan(count), all = __builtin_amdgcn_readlane(upto, 63);
+    if (all == 0) return;
+    int at = 0;
+    if (lane == 0) at = atomicAdd(&S.n, all);
+    at = __builtin_amdgcn_readfirstlane(at);
+    if (at + all > LIST) return;  // seen below, by every thread
+    at += upto - count;
+#pragma unroll
+    for (int j = 0; j < NE; ++j)
+      if (mine >> j & 1) {
+        float z;
+        int c;
+        get(j, z, c);
+        S.list[at++] = entry(z, c);
+      }
+  };
+  static_assert(NE <= 32, "a bit for each logit");
+  if (many || wave_hits) list([&](float z, int) { return z >= from; });
   __syncthreads();
-  n = S.n;
-  if (n >= K + SLACK || many) {
-    __syncthreads();  // S.n has been read
-    n = cut(S, n, K);
+  if (many && S.n > LIST) {
+    // the K-th best logit of the chunk, and of those equal to it the lowest classes
+    const int most = LIST - p.n;
+    __syncthreads();
+    if (threadIdx.x == 0) S.n = p.n;
+    auto reach = [&](float x, uint32_t last) {
+      __asm__ volatile("" : "+v"(x));  // keeps the comparisons of a rare path out of the registers of the common one
+      int n = 0;
+#pragma unroll
+      for (int j = 0; j < NE; ++j) {
+        float z;
+        int c;
+        get(j, z, c);
+        n += (int)__popcll(__ballot(z > x || (z == x && uint32_t(c) <= last)));
+      }
+      return block_count<NT>(n, S.count);
+    };
+    const float kth = key_logit(search(K, most, [&](uint32_t k) { return reach(fmaxf(from, key_logit(k)), ~0u); }));
+    from = fmaxf(from, kth);
+    const uint32_t last = ~search(K, most, [&](uint32_t k) { return reach(from, ~k); });
+    __syncthreads();
+    list([&](float z, int c) { return z > from || (z == from && uint32_t(c) <= last); });
+    __syncthreads();
   }
-  if (n == K && K > 0) bar = entry_logit(S.list[K - 1]);
+  p.n = S.n;
+  p.sorted = false;
+  if (p.n >= K + SLACK || many) {
+    __syncthreads();  // S.n has been read
+    cut(S, p, K);
+  }
+  if (p.sorted && p.n == K) p.bar = entry_logit(S.list[K - 1]);
 }
 
 template <int NT>
@@ -221,11 +271,10 @@ __global__ void __launch_bounds__(NT) k_logprob(LogprobArgs a, int segs, int seg
     const T* z = static_cast<const T*>(a.z) + row * a.ld;
     select_begin(S);
     RowStats<true> st;
-    float bar = -INFINITY;
-    int n = 0, turn = 0;
+    Progress p;
     u32x4 v[NV], next[NV];
     row_chunk<T, NT, NV>(z, first, end, v);
-    for (int64_t from = first; from < end; from += CHUNK, ++turn) {
+    for (int64_t from = first; from < end; from += CHUNK) {
       const bool more = from + CHUNK < end;
       if (more) row_chunk<T, NT, NV>(z, from + CHUNK, end, next);
       float best = -INFINITY;
@@ -240,25 +289,28 @@ __global__ void __launch_bounds__(NT) k_logprob(LogprobArgs a, int segs, int seg
         for (int e = 0; e < VEC; ++e) st.add(RT::get(v[j], e), LOG2E);
       if (a.K > 0) {
         const int base = (int)from + (int)threadIdx.x * VEC;
-        select_chunk<NT, NE>(S, a.K, best, [&](int j, float& x, int& c) {
-          x = RT::get(v[j / VEC], j % VEC);
-          c = base + j / VEC * NT * VEC + j % VEC;
-        }, bar, n, turn);
+        select_chunk<NT, NE>(S, p, a.K, best, [&](int j, float& x, int& c) {
+          int at = base;
+          u32x4 raw = v[j / VEC];
+          __asm__ volatile("" : "+v"(at), "+v"(raw));  // classes and fp32 logits are formed where they are used, not kept
+          x = RT::get(raw, j % VEC);
+          c = at + j / VEC * NT * VEC + j % VEC;
+        });
       }
       if (more)
 #pragma unroll
         for (int j = 0; j < NV; ++j) v[j] = next[j];
     }
     __syncthreads();
-    if (a.K > 0) n = cut(S, n, a.K);
+    cut(S, p, a.K);
     st.over_block<NT>(LOG2E, sh);
     if constexpr (SPLIT) {
       Part* part = static_cast<Part*>(a.scratch) + item;
       uint64_t* list = reinterpret_cast<uint64_t*>(static_cast<Part*>(a.scratch) + items) + item * a.K;
-      if (threadIdx.x == 0) *part = Part{st.m, st.s, st.t, n};
-      for (int i = threadIdx.x; i < a.K; i += NT) list[i] = i < n ? S.list[i] : 0;
+      if (threadIdx.x == 0) *part = Part{st.m, st.s, st.t, p.n};
+      for (int i = threadIdx.x; i < a.K; i += NT) list[i] = i < p.n ? S.list[i] : 0;
     } else {
-      write_row<T, NT>(a, row, z, st, S, n);
+      write_row<T, NT>(a, row, z, st, S, p.n);
     }
     __syncthreads();
   }
@@ -286,11 +338,10 @@ __global__ void __launch_bounds__(JOIN_T) k_logprob_join(LogprobArgs a, int segs
     st.s += q.s;
     st.t += q.t;
   }
-  float bar = -INFINITY;
-  int n = 0, turn = 0;
+  Progress p;
   // equal logits in later entries have higher classes, as select_chunk's bar needs: segments
   // are in the order of their classes, and so are equal logits inside one
-  for (int from = 0; from < segs * a.K; from += JOIN_T * JOIN_E, ++turn) {
+  for (int from = 0; from < segs * a.K; from += JOIN_T * JOIN_E) {
     uint64_t e[JOIN_E];
     float best = -INFINITY;
 #pragma unroll
@@ -299,15 +350,15 @@ __global__ void __launch_bounds__(JOIN_T) k_logprob_join(LogprobArgs a, int segs
       e[j] = i < segs * a.K ? list[i] : 0;
       if (e[j]) best = fmaxf(best, entry_logit(e[j]));
     }
-    select_chunk<JOIN_T, JOIN_E>(S, a.K, best, [&](int j, float& x, int& c) {
+    select_chunk<JOIN_T, JOIN_E>(S, p, a.K, best, [&](int j, float& x, int& c) {
       x = e[j] ? entry_logit(e[j]) : -INFINITY;
       c = entry_class(e[j]);
-    }, bar, n, turn);
+    });
   }
   __syncthreads();
-  if (a.K > 0) n = cut(S, n, a.K);
+  cut(S, p, a.K);
   st.over_block<JOIN_T>(LOG2E, sh);
-  write_row<T, JOIN_T>(a, row, static_cast<const T*>(a.z) + row * a.ld, st, S, n);
+  write_row<T, JOIN_T>(a, row, static_cast<const T*>(a.z) + row * a.ld, st, S, p.n);
 }
 
 template <class T>

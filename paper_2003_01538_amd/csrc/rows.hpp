@@ -77,9 +77,40 @@ __device__ __forceinline__ void row_chunk(const T* z, int64_t from, int64_t end,
   }
 }
 
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+// Wavefront reductions in registers: within rows of 16 lanes, then a row's last
+// lane to the next row, then the lower half's to the upper; lane 63 has all.  Six
+// steps of a few cycles each, where a shuffle through LDS takes some 60.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float dpp(float keep, float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(keep), __float_as_int(v), CTRL, ROWS, 0xf, false));
+}
+__device__ __forceinline__ float row_wave_max(float v) {
+  v = fmaxf(v, dpp<0x111, 0xf>(v, v));  // row_shr 1, 2, 4, 8
+  v = fmaxf(v, dpp<0x112, 0xf>(v, v));
+  v = fmaxf(v, dpp<0x114, 0xf>(v, v));
+  v = fmaxf(v, dpp<0x118, 0xf>(v, v));
+  v = fmaxf(v, dpp<0x142, 0xa>(v, v));  // row_bcast 15 into rows 1 and 3
+  v = fmaxf(v, dpp<0x143, 0xc>(v, v));  // row_bcast 31 into rows 2 and 3
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+__device__ __forceinline__ float row_wave_sum(float v) {
+  v += dpp<0x111, 0xf>(0.f, v);
+  v += dpp<0x112, 0xf>(0.f, v);
+  v += dpp<0x114, 0xf>(0.f, v);
+  v += dpp<0x118, 0xf>(0.f, v);
+  v += dpp<0x142, 0xa>(0.f, v);
+  v += dpp<0x143, 0xc>(0.f, v);
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
+// Sum over the lanes up to this one.
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
   return v;
 }
 
@@ -87,7 +118,7 @@ __device__ __forceinline__ float wave_max(float v) {
 // holds one value per wave and is free again after the call.
 template <int NT>
 __device__ __forceinline__ float block_sum(float v, float* sh) {
-  v = wave_sum(v);
+  v = row_wave_sum(v);
   if constexpr (NT > 64) {
     if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
     __syncthreads();
@@ -100,7 +131,7 @@ __device__ __forceinline__ float block_sum(float v, float* sh) {
 }
 template <int NT>
 __device__ __forceinline__ float block_max(float v, float* sh) {
-  v = wave_max(v);
+  v = row_wave_max(v);
   if constexpr (NT > 64) {
     if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
     __syncthreads();
