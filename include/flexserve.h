@@ -464,7 +464,8 @@ typedef enum { FS_ACT_NONE = 0, FS_ACT_RELU = 1, FS_ACT_GELU = 2, FS_ACT_SILU = 
  * or FS_BF16 for bf16 x and w.  Sums, bias, activation and residual are fp32
  * and rounded once.  K = 0 is an empty sum.
  * FS_ERR_INVALID for NULL, negative sizes or rows that are too near;
- * FS_ERR_UNSUPPORTED for bf16 output of fp32 inputs. */
+ * FS_ERR_UNSUPPORTED for bf16 output of fp32 inputs, M or N beyond 2^26, K
+ * beyond 2^30. */
 fs_status fs_linear_device(const void *d_x, int64_t ldx, const void *d_w, int64_t ldw, const float *d_bias,
                            const void *d_res, int64_t ldres, void *d_y, int64_t ldy, int32_t M, int32_t N,
                            int32_t K, int32_t precision, int32_t out_precision, int32_t activation,

@@ -1,74 +1,353 @@
 // Matrix product with bias, activation and residual on a caller's tensors:
 // y[m][n] = act(sum_k x[m][k] w[n][k] + bias[n] (+ res)) (+ res).
 //
-// A workgroup makes a 64 x 64 tile of y: 16-wide slices of its rows of x and w
-// go through LDS as fp32, each thread sums a 4 x 4 patch.
+// Two kernels.  k_linear_few is for outputs of few tiles: a workgroup makes a
+// small tile and its waves split the reduction, each loading its operands
+// straight into registers (nothing is shared, so nothing is staged), and their
+// sums meet in LDS in wave order.  k_linear_tile is for many tiles: operands go
+// through LDS, each wave sums its part of the tile over the whole reduction.
+//
+// Both take rows at any distance and alignment; which of them and with which
+// tile runs is a rule on sizes and alignment (launch_linear).
+//
+// MFMA operands: A = weights, B = x, so that a lane's accumulators hold
+// consecutive features n of one row m.  The order of k inside a 16-byte piece
+// and between the pieces of a step is free as long as both operands share it.
 #include "common.hpp"
 #include "device.hpp"
+#include "lds_dma.hpp"
 
 #include "flexserve.h"
+
+#include <algorithm>
 
 namespace fs {
 
 namespace {
 
-__device__ __forceinline__ float load_f(const float* p) { return *p; }
-__device__ __forceinline__ float load_f(const uint16_t* p) { return bf2f(*p); }
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef u32x4 u32x4_at2 __attribute__((aligned(2)));
+typedef u32x2 u32x2_at2 __attribute__((aligned(2)));
+typedef floatx4 floatx4_at4 __attribute__((aligned(4)));
 
-// bias, residual, activation and the one rounding of output (m, n)
-__device__ __forceinline__ void linear_store(const LinearArgs& a, int m, int n, float v) {
-  if (a.bias) v += a.bias[n];
-  float r = 0.f;
-  if (a.res) {
-    const int64_t o = (int64_t)m * a.ldres + n;
-    r = a.out_f32 ? static_cast<const float*>(a.res)[o] : bf2f(static_cast<const uint16_t*>(a.res)[o]);
+template <class T> struct LinT;
+template <> struct LinT<uint16_t> {  // bf16
+  static constexpr int VEC = 8;
+  static __device__ __forceinline__ floatx4 mma16(u32x4 w, u32x4 x, floatx4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, x), c, 0, 0, 0);
   }
-  if (a.res_first) v += r;
-  if (a.act == FS_ACT_RELU) v = v > 0.f ? v : 0.f;
-  else if (a.act == FS_ACT_GELU) v = 0.5f * v * (1.f + erff(v * 0.70710678f));
-  else if (a.act == FS_ACT_SILU) v = v / (1.f + expf(-v));
-  if (!a.res_first && a.res) v += r;
-  const int64_t o = (int64_t)m * a.ldy + n;
-  if (a.out_f32) static_cast<float*>(a.y)[o] = v;
-  else static_cast<uint16_t*>(a.y)[o] = f2bf(v);
+  static __device__ __forceinline__ floatx16 mma32(u32x4 w, u32x4 x, floatx16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, w), __builtin_bit_cast(bf16x8, x), c, 0, 0, 0);
+  }
+};
+template <> struct LinT<float> {
+  static constexpr int VEC = 4;
+  static __device__ __forceinline__ floatx4 mma16(u32x4 w, u32x4 x, floatx4 c) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[e]), __uint_as_float(x[e]), c, 0, 0, 0);
+    return c;
+  }
+  static __device__ __forceinline__ floatx16 mma32(u32x4 w, u32x4 x, floatx16 c) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(w[e]), __uint_as_float(x[e]), c, 0, 0, 0);
+    return c;
+  }
+};
+
+// 16 bytes of a row at any element (the hardware takes vector accesses at every
+// byte address); zeros behind its end.
+template <class T>
+__device__ __forceinline__ u32x4 piece(const T* row, int k, int K) {
+  constexpr int VEC = LinT<T>::VEC;
+  if (k + VEC <= K) return *reinterpret_cast<const u32x4_at2*>(row + k);
+  T t[VEC];
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) t[e] = k + e < K ? row[k + e] : T(0);
+  return __builtin_bit_cast(u32x4, t);
+}
+
+__device__ __forceinline__ float activate(float v, int act) {
+  if (act == FS_ACT_RELU) return v > 0.f ? v : 0.f;
+  if (act == FS_ACT_GELU) return 0.5f * v * (1.f + erff(v * 0.70710678f));
+  if (act == FS_ACT_SILU) return v / (1.f + expf(-v));
+  return v;
+}
+
+// bias, residual, activation and the one rounding of outputs (m, n .. n + 3),
+// those that exist
+__device__ __forceinline__ void finish4(const LinearArgs& a, int m, int n, floatx4 v) {
+  if (m >= a.M || n >= a.N) return;
+  const int64_t o = (int64_t)m * a.ldy + n, ro = (int64_t)m * a.ldres + n;
+  if (n + 4 <= a.N) {
+    if (a.bias) {
+      const floatx4 b = *reinterpret_cast<const floatx4_at4*>(a.bias + n);
+      v += b;
+    }
+    floatx4 r = {0.f, 0.f, 0.f, 0.f};
+    if (a.res) {
+      if (a.out_f32) {
+        r = *reinterpret_cast<const floatx4_at4*>(static_cast<const float*>(a.res) + ro);
+      } else {
+        const u32x2 q = *reinterpret_cast<const u32x2_at2*>(static_cast<const uint16_t*>(a.res) + ro);
+        r = floatx4{__uint_as_float(q[0] << 16), __uint_as_float(q[0] & 0xffff0000u), __uint_as_float(q[1] << 16),
+                    __uint_as_float(q[1] & 0xffff0000u)};
+      }
+      if (a.res_first) v += r;
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = activate(v[e], a.act);
+    if (a.res && !a.res_first) v += r;
+    if (a.out_f32) {
+      *reinterpret_cast<floatx4_at4*>(static_cast<float*>(a.y) + o) = v;
+    } else {
+      *reinterpret_cast<u32x2_at2*>(static_cast<uint16_t*>(a.y) + o) =
+          u32x2{f2bf(v[0]) | uint32_t(f2bf(v[1])) << 16, f2bf(v[2]) | uint32_t(f2bf(v[3])) << 16};
+    }
+    return;
+  }
+  for (int e = 0; n + e < a.N; ++e) {
+    float s = v[e];
+    if (a.bias) s += a.bias[n + e];
+    float r = 0.f;
+    if (a.res) r = a.out_f32 ? static_cast<const float*>(a.res)[ro + e] : bf2f(static_cast<const uint16_t*>(a.res)[ro + e]);
+    if (a.res && a.res_first) s += r;
+    s = activate(s, a.act);
+    if (a.res && !a.res_first) s += r;
+    if (a.out_f32) static_cast<float*>(a.y)[o + e] = s;
+    else static_cast<uint16_t*>(a.y)[o + e] = f2bf(s);
+  }
+}
+
+// --------------------------------------------------------------- few tiles
+// A tile of 16 FN features x 16 FM rows.  Step s of the reduction is a run of
+// 128 bytes of each row: lane group g = lane / 16 takes 32 of them in two
+// pieces, so that a step's loads use whole cache lines.  Wave w takes steps w,
+// w + NW, ..., U of them in flight.
+template <class T, int FM, int FN, int NW, int U>
+__global__ void __launch_bounds__(NW * 64) k_linear_few(LinearArgs a) {
+  using L = LinT<T>;
+  constexpr int VEC = L::VEC, STEP = 8 * VEC;
+  __shared__ floatx4 part[NW][FM * FN][64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int tiles_n = (a.N + 16 * FN - 1) / (16 * FN);
+  const int n0 = blockIdx.x % tiles_n * (16 * FN), m0 = blockIdx.x / tiles_n * (16 * FM);
+  const int off = (lane >> 4) * 2 * VEC;
+  // rows that do not exist read row 0: they enter only outputs that do not exist
+  const T* wr[FN];
+  const T* xr[FM];
+#pragma unroll
+  for (int j = 0; j < FN; ++j) {
+    const int n = n0 + j * 16 + (lane & 15);
+    wr[j] = static_cast<const T*>(a.w) + (int64_t)(n < a.N ? n : 0) * a.ldw;
+  }
+#pragma unroll
+  for (int i = 0; i < FM; ++i) {
+    const int m = m0 + i * 16 + (lane & 15);
+    xr[i] = static_cast<const T*>(a.x) + (int64_t)(m < a.M ? m : 0) * a.ldx;
+  }
+  floatx4 acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+  u32x4 w[U][FN][2], x[U][FM][2];
+  auto products = [&](int u) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = L::mma16(w[u][j][h], x[u][i][h], acc[i][j]);
+  };
+  int k = wave * STEP;
+  for (; k + (U - 1) * NW * STEP + STEP <= a.K; k += U * NW * STEP) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int ku = k + u * NW * STEP + off;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j) w[u][j][h] = *reinterpret_cast<const u32x4_at2*>(wr[j] + ku + h * VEC);
+#pragma unroll
+        for (int i = 0; i < FM; ++i) x[u][i][h] = *reinterpret_cast<const u32x4_at2*>(xr[i] + ku + h * VEC);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);  // all loads are under way before the first product waits
+#pragma unroll
+    for (int u = 0; u < U; ++u) products(u);
+  }
+  for (; k < a.K; k += NW * STEP) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int j = 0; j < FN; ++j) w[0][j][h] = piece(wr[j], k + off + h * VEC, a.K);
+#pragma unroll
+      for (int i = 0; i < FM; ++i) x[0][i][h] = piece(xr[i], k + off + h * VEC, a.K);
+    }
+    products(0);
+  }
+
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) part[wave][i * FN + j][lane] = acc[i][j];
+  __syncthreads();
+  // block (i, j): lane l holds row l % 16 and features 4 (l / 16) ..
+  for (int t = tid; t < FM * FN * 64; t += NW * 64) {
+    const int b = t >> 6, l = t & 63;
+    floatx4 s = part[0][b][l];
+#pragma unroll
+    for (int q = 1; q < NW; ++q) s += part[q][b][l];
+    finish4(a, m0 + b / FN * 16 + (l & 15), n0 + b % FN * 16 + (l >> 4) * 4, s);
+  }
+}
+
+// -------------------------------------------------------------- many tiles
+// A tile of BM rows x BN features on WM x WN waves.  K-tiles of 128 bytes a row
+// lie in LDS as in lds_dma.hpp, two of them in turn: while one is used, the next
+// is on its way.  DMA: the loads write LDS themselves (rows aligned to 16 bytes);
+// otherwise they pass through registers.
+template <class T, int BM, int BN, int WM, int WN, bool DMA>
+__global__ void __launch_bounds__(WM * WN * 64) k_linear_tile(LinearArgs a) {
+  using L = LinT<T>;
+  constexpr int VEC = L::VEC, KT = 8 * VEC, NT = WM * WN * 64, ES = sizeof(T);
+  constexpr int FM = BM / WM / 32, FN = BN / WN / 32;
+  constexpr int PA = BM * 8 / NT, PB = BN * 8 / NT;  // 16-byte pieces of a K-tile per thread
+  __shared__ __attribute__((aligned(1024))) char lds[2][(BM + BN) * ROW];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int wm = wave / WN, wn = wave % WN;
+
+  // consecutive tiles on one XCD, in groups of 8 tile rows, so that its L2 serves a
+  // block of tiles whose operands it holds
+  const int tiles_m = (a.M + BM - 1) / BM, tiles_n = (a.N + BN - 1) / BN;
+  const int id = xcd_remap(blockIdx.x, gridDim.x);
+  const int group = id / (8 * tiles_n), in = id - group * 8 * tiles_n;
+  const int rows = min(8, tiles_m - group * 8);
+  const int m0 = (group * 8 + in % rows) * BM, n0 = in / rows * BN;
+
+  // thread t, piece p: tile row (p NT + t) / 8, physical chunk t % 8
+  const int prow = tid >> 3;
+  const T* xb = static_cast<const T*>(a.x) + (int64_t)m0 * a.ldx;
+  const T* wb = static_cast<const T*>(a.w) + (int64_t)n0 * a.ldw;
+  const int steps = (a.K + KT - 1) / KT;
+
+  u32x4 ra[DMA ? 1 : PA], rb[DMA ? 1 : PB];
+  const __amdgpu_buffer_rsrc_t rx = rsrc(xb, DMA ? (uint32_t)((int64_t)(min(BM, a.M - m0) - 1) * a.ldx * ES + (int64_t)a.K * ES) : 0u);
+  const __amdgpu_buffer_rsrc_t rw = rsrc(wb, DMA ? (uint32_t)((int64_t)(min(BN, a.N - n0) - 1) * a.ldw * ES + (int64_t)a.K * ES) : 0u);
+  auto fetch = [&](int s, int buf) {
+    const int k0 = s * KT;
+#pragma unroll
+    for (int p = 0; p < PA + PB; ++p) {
+      const bool is_a = p < PA;
+      const int r = prow + (is_a ? p : p - PA) * (NT / 8);
+      const int k = k0 + (((tid & 7) ^ swz(r)) * VEC);
+      const bool ok = is_a ? m0 + r < a.M : n0 + r < a.N;
+      if constexpr (DMA) {
+        const uint32_t o = ok && k < a.K ? (uint32_t)((int64_t)r * (is_a ? a.ldx : a.ldw) + k) * ES : OOB;
+        char* to = lds[buf] + (is_a ? 0 : BM * ROW) + ((is_a ? p : p - PA) * NT + wave * 64) * 16;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(is_a ? rx : rw, (lds_void*)to, 16, o, 0, 0, 0);
+      } else {
+        const u32x4 q = ok ? piece((is_a ? xb + (int64_t)r * a.ldx : wb + (int64_t)r * a.ldw), k, a.K) : u32x4{0, 0, 0, 0};
+        if (is_a) ra[p] = q;
+        else rb[p - PA] = q;
+      }
+    }
+  };
+  auto store = [&](int buf) {
+    if constexpr (!DMA) {
+#pragma unroll
+      for (int p = 0; p < PA; ++p) *reinterpret_cast<u32x4*>(lds[buf] + (p * NT + tid) * 16) = ra[p];
+#pragma unroll
+      for (int p = 0; p < PB; ++p) *reinterpret_cast<u32x4*>(lds[buf] + BM * ROW + (p * NT + tid) * 16) = rb[p];
+    }
+  };
+
+  floatx16 acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+
+  const int fr = lane & 31, fq = lane >> 5;
+  if (steps > 0) fetch(0, 0);
+  for (int s = 0; s < steps; ++s) {
+    const int buf = s & 1;
+    if constexpr (DMA) {
+      wait_vmcnt<0>();  // this wave's part of the K-tile is in LDS
+      wg_barrier();     // every wave's is, and the other buffer is free
+      if (s + 1 < steps) fetch(s + 1, buf ^ 1);
+    } else {
+      store(buf);
+      __syncthreads();
+      if (s + 1 < steps) fetch(s + 1, buf ^ 1);
+    }
+    const char* A = lds[buf] + (wm * FM * 32 + fr) * ROW;
+    const char* B = lds[buf] + BM * ROW + (wn * FN * 32 + fr) * ROW;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+      const int c = ((ks * 2 + fq) ^ swz(fr)) << 4;
+      u32x4 xf[FM], wf[FN];
+#pragma unroll
+      for (int i = 0; i < FM; ++i) xf[i] = *reinterpret_cast<const u32x4*>(A + i * 32 * ROW + c);
+#pragma unroll
+      for (int j = 0; j < FN; ++j) wf[j] = *reinterpret_cast<const u32x4*>(B + j * 32 * ROW + c);
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = L::mma32(wf[j], xf[i], acc[i][j]);
+    }
+  }
+
+  // block (i, j): lane l holds row l % 32 and features 8 g + 4 (l / 32) .. of g = 0 .. 3
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        finish4(a, m0 + (wm * FM + i) * 32 + fr, n0 + (wn * FN + j) * 32 + 8 * g + 4 * fq,
+                floatx4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]});
+}
+
+template <class T, int FM, int FN, int NW, int U>
+void few(const LinearArgs& a, hipStream_t s) {
+  const int64_t tiles = (int64_t)((a.N + 16 * FN - 1) / (16 * FN)) * ((a.M + 16 * FM - 1) / (16 * FM));
+  hipLaunchKernelGGL((k_linear_few<T, FM, FN, NW, U>), dim3((unsigned)tiles), dim3(NW * 64), 0, s, a);
+}
+
+template <class T, int BM, int BN, int WM, int WN>
+void tile(const LinearArgs& a, bool dma, hipStream_t s) {
+  const int64_t tiles = (int64_t)((a.N + BN - 1) / BN) * ((a.M + BM - 1) / BM);
+  if (dma) hipLaunchKernelGGL((k_linear_tile<T, BM, BN, WM, WN, true>), dim3((unsigned)tiles), dim3(WM * WN * 64), 0, s, a);
+  else hipLaunchKernelGGL((k_linear_tile<T, BM, BN, WM, WN, false>), dim3((unsigned)tiles), dim3(WM * WN * 64), 0, s, a);
 }
 
 template <class T>
-__global__ void __launch_bounds__(256) k_linear(LinearArgs a) {
-  __shared__ float xs[16][65], ws[16][65];
-  const int tiles_n = (a.N + 63) / 64;
-  const int m0 = blockIdx.x / tiles_n * 64, n0 = blockIdx.x % tiles_n * 64;
-  const int tid = threadIdx.x, tm = tid / 16 * 4, tn = tid % 16 * 4;
-  const T* x = static_cast<const T*>(a.x);
-  const T* w = static_cast<const T*>(a.w);
-  float acc[4][4] = {};
-  for (int k0 = 0; k0 < a.K; k0 += 16) {
-    for (int i = tid; i < 64 * 16; i += 256) {
-      const int r = i / 16, k = k0 + i % 16;
-      xs[i % 16][r] = k < a.K && m0 + r < a.M ? load_f(x + (int64_t)(m0 + r) * a.ldx + k) : 0.f;
-      ws[i % 16][r] = k < a.K && n0 + r < a.N ? load_f(w + (int64_t)(n0 + r) * a.ldw + k) : 0.f;
-    }
-    __syncthreads();
-    for (int k = 0; k < 16; ++k)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(xs[k][tm + i], ws[k][tn + j], acc[i][j]);
-    __syncthreads();
-  }
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (m0 + tm + i < a.M && n0 + tn + j < a.N) linear_store(a, m0 + tm + i, n0 + tn + j, acc[i][j]);
+void launch_t(const LinearArgs& a, hipStream_t s) {
+  constexpr int VEC = LinT<T>::VEC;
+  // the loads that write LDS move 16 aligned bytes, at 31-bit offsets from a tile's first row
+  const bool dma = a.K % VEC == 0 && a.ldx % VEC == 0 && a.ldw % VEC == 0 && reinterpret_cast<uintptr_t>(a.x) % 16 == 0 &&
+                   reinterpret_cast<uintptr_t>(a.w) % 16 == 0 && std::max(a.ldx, a.ldw) < (int64_t(1) << 31) / (256 * (int64_t)sizeof(T)) - a.K;
+  auto tiles = [&](int64_t bm, int64_t bn) { return (a.M + bm - 1) / bm * ((a.N + bn - 1) / bn); };
+  if (a.M <= 16) return few<T, 1, 1, 8, 4>(a, s);
+  if (a.M <= 32) return few<T, 2, 1, 8, 4>(a, s);
+  if (tiles(64, 64) < 128) return few<T, 2, 2, 8, 2>(a, s);
+  if (tiles(256, 256) >= 200) return tile<T, 256, 256, 2, 4>(a, dma, s);
+  if (tiles(128, 128) >= 200) return tile<T, 128, 128, 2, 2>(a, dma, s);
+  return tile<T, 64, 64, 2, 2>(a, dma, s);
 }
 
 }  // namespace
 
 void launch_linear(const LinearArgs& a, Prec p, hipStream_t s) {
-  const int64_t tiles = (int64_t)((a.M + 63) / 64) * ((a.N + 63) / 64);
-  if (p == BF16) hipLaunchKernelGGL(k_linear<uint16_t>, dim3((unsigned)tiles), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(k_linear<float>, dim3((unsigned)tiles), dim3(256), 0, s, a);
+  if (p == BF16) launch_t<uint16_t>(a, s);
+  else launch_t<float>(a, s);
 }
 
 }  // namespace fs

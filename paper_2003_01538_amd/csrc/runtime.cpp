@@ -1739,6 +1739,7 @@ fs_status fs_linear_device(const void* d_x, int64_t ldx, const void* d_w, int64_
     if (precision == FS_F32 && out_precision != FS_F32) fail(FS_ERR_UNSUPPORTED, "fp32 inputs give fp32 output");
     if (activation < FS_ACT_NONE || activation > FS_ACT_SILU) fail(FS_ERR_INVALID, "unknown activation");
     if (M < 0 || N < 0 || K < 0) fail(FS_ERR_INVALID, "sizes must be >= 0");
+    if (M > 1 << 26 || N > 1 << 26 || K > 1 << 30) fail(FS_ERR_UNSUPPORTED, "M and N up to 2^26, K up to 2^30");
     if (ldx < K || ldw < K || ldy < N || (d_res && ldres != 0 && ldres < N))
       fail(FS_ERR_INVALID, "a row distance is shorter than its row");
     if (M == 0 || N == 0) return;

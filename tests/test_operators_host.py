@@ -35,6 +35,7 @@ def status(fn, base, **change):
     (dict(res=P, ldres=-4), INV), (dict(prec=2), INV), (dict(out=2), INV), (dict(act=4), INV), (dict(act=-1), INV),
     (dict(prec=F, out=BF), UNS), (dict(x=P + 1), INV), (dict(bias=P + 2), INV), (dict(y=P + 2), INV),
     (dict(res=P, ldres=5), INV),  # over the output with another row distance
+    (dict(M=(1 << 26) + 1), UNS), (dict(N=(1 << 26) + 1, ldy=1 << 27), UNS), (dict(K=(1 << 30) + 1, ldx=1 << 31, ldw=1 << 31), UNS),
     (dict(M=0, x=None), fsb.FS_OK), (dict(N=0, ldy=0, w=None), fsb.FS_OK),
 ])
 def test_linear_refuses(change, want):
