@@ -208,17 +208,24 @@ __global__ void __launch_bounds__(NW * 64) k_linear_few(LinearArgs a) {
 
 // -------------------------------------------------------------- many tiles
 // A tile of BM rows x BN features on WM x WN waves.  K-tiles of 128 bytes a row
-// lie in LDS as in lds_dma.hpp, two of them in turn: while one is used, the next
-// is on its way.  DMA: the loads write LDS themselves (rows aligned to 16 bytes);
-// otherwise they pass through registers.
+// lie in LDS as in lds_dma.hpp, two of them in turn.  DMA: the loads write LDS
+// themselves (rows aligned to 16 bytes); otherwise they pass through registers.
+//
+// A K-tile is four steps of MFMAs.  The operands of a step are read from LDS during
+// the step before it; the barrier between two K-tiles lies before the last step,
+// whose operands are in registers by then, so the matrix cores have work while
+// the waves meet and the next K-tile's first operands are read.
 template <class T, int BM, int BN, int WM, int WN, bool DMA>
 __global__ void __launch_bounds__(WM * WN * 64) k_linear_tile(LinearArgs a) {
   using L = LinT<T>;
   constexpr int VEC = L::VEC, KT = 8 * VEC, NT = WM * WN * 64, ES = sizeof(T);
   constexpr int FM = BM / WM / 32, FN = BN / WN / 32;
   constexpr int PA = BM * 8 / NT, PB = BN * 8 / NT;  // 16-byte pieces of a K-tile per thread
-  __shared__ __attribute__((aligned(1024))) char lds[2][(BM + BN) * ROW];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  constexpr int BUF = (BM + BN) * ROW;
+  constexpr int PITCH = BN + 4;  // floats of a row of the finished tile
+  static_assert(WM * 32 * PITCH * 4 <= 2 * BUF, "a row block of the finished tile fits where the operands were");
+  __shared__ __attribute__((aligned(1024))) char lds[2 * BUF];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave / WN, wn = wave % WN;
 
   // consecutive tiles on one XCD, in groups of 8 tile rows, so that its L2 serves a
@@ -228,41 +235,49 @@ __global__ void __launch_bounds__(WM * WN * 64) k_linear_tile(LinearArgs a) {
   const int group = id / (8 * tiles_n), in = id - group * 8 * tiles_n;
   const int rows = min(8, tiles_m - group * 8);
   const int m0 = (group * 8 + in % rows) * BM, n0 = in / rows * BN;
-
-  // thread t, piece p: tile row (p NT + t) / 8, physical chunk t % 8
-  const int prow = tid >> 3;
   const T* xb = static_cast<const T*>(a.x) + (int64_t)m0 * a.ldx;
   const T* wb = static_cast<const T*>(a.w) + (int64_t)n0 * a.ldw;
   const int steps = (a.K + KT - 1) / KT;
 
-  u32x4 ra[DMA ? 1 : PA], rb[DMA ? 1 : PB];
-  const __amdgpu_buffer_rsrc_t rx = rsrc(xb, DMA ? (uint32_t)((int64_t)(min(BM, a.M - m0) - 1) * a.ldx * ES + (int64_t)a.K * ES) : 0u);
-  const __amdgpu_buffer_rsrc_t rw = rsrc(wb, DMA ? (uint32_t)((int64_t)(min(BN, a.N - n0) - 1) * a.ldw * ES + (int64_t)a.K * ES) : 0u);
-  auto fetch = [&](int s, int buf) {
-    const int k0 = s * KT;
+  // thread t, piece p: tile row p NT / 8 + t / 8, physical chunk t % 8; the rows of a
+  // thread's pieces share their swizzle (NT / 8 is a multiple of 16)
+  static_assert(NT / 8 % 16 == 0, "rows of one swizzle");
+  const int prow = tid >> 3, kc = ((tid & 7) ^ swz(prow)) * VEC;
+  const __amdgpu_buffer_rsrc_t rx = rsrc(xb, DMA ? (uint32_t)(((min(BM, a.M - m0) - 1) * a.ldx + a.K) * ES) : 0u);
+  const __amdgpu_buffer_rsrc_t rw = rsrc(wb, DMA ? (uint32_t)(((min(BN, a.N - n0) - 1) * a.ldw + a.K) * ES) : 0u);
+  uint32_t off[DMA ? PA + PB : 1];
+  u32x4 reg[DMA ? 1 : PA + PB];
+  if constexpr (DMA) {
 #pragma unroll
     for (int p = 0; p < PA + PB; ++p) {
-      const bool is_a = p < PA;
-      const int r = prow + (is_a ? p : p - PA) * (NT / 8);
-      const int k = k0 + (((tid & 7) ^ swz(r)) * VEC);
-      const bool ok = is_a ? m0 + r < a.M : n0 + r < a.N;
-      if constexpr (DMA) {
-        const uint32_t o = ok && k < a.K ? (uint32_t)((int64_t)r * (is_a ? a.ldx : a.ldw) + k) * ES : OOB;
-        char* to = lds[buf] + (is_a ? 0 : BM * ROW) + ((is_a ? p : p - PA) * NT + wave * 64) * 16;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(is_a ? rx : rw, (lds_void*)to, 16, o, 0, 0, 0);
-      } else {
-        const u32x4 q = ok ? piece((is_a ? xb + (int64_t)r * a.ldx : wb + (int64_t)r * a.ldw), k, a.K) : u32x4{0, 0, 0, 0};
-        if (is_a) ra[p] = q;
-        else rb[p - PA] = q;
+      const int r = prow + (p < PA ? p : p - PA) * (NT / 8);
+      const bool ok = p < PA ? m0 + r < a.M : n0 + r < a.N;
+      off[p] = ok ? (uint32_t)((r * (p < PA ? a.ldx : a.ldw) + kc) * ES) : OOB;  // stays out of range with any k added
+    }
+  }
+  auto fetch = [&](int s, int buf) {
+    const int k0 = s * KT;
+    if constexpr (DMA) {
+      const uint32_t kb = k0 + kc < a.K ? (uint32_t)(k0 * ES) : OOB;
+#pragma unroll
+      for (int p = 0; p < PA + PB; ++p) {
+        char* to = lds + buf * BUF + (p * NT + wave * 64) * 16;
+        const uint32_t o = max(off[p], kb) == OOB ? OOB : off[p] + kb;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(p < PA ? rx : rw, (lds_void*)to, 16, o, 0, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int p = 0; p < PA + PB; ++p) {
+        const int r = prow + (p < PA ? p : p - PA) * (NT / 8);
+        const bool ok = p < PA ? m0 + r < a.M : n0 + r < a.N;
+        reg[p] = ok ? piece(p < PA ? xb + r * a.ldx : wb + r * a.ldw, k0 + kc, a.K) : u32x4{0, 0, 0, 0};
       }
     }
   };
   auto store = [&](int buf) {
     if constexpr (!DMA) {
 #pragma unroll
-      for (int p = 0; p < PA; ++p) *reinterpret_cast<u32x4*>(lds[buf] + (p * NT + tid) * 16) = ra[p];
-#pragma unroll
-      for (int p = 0; p < PB; ++p) *reinterpret_cast<u32x4*>(lds[buf] + BM * ROW + (p * NT + tid) * 16) = rb[p];
+      for (int p = 0; p < PA + PB; ++p) *reinterpret_cast<u32x4*>(lds + buf * BUF + (p * NT + tid) * 16) = reg[p];
     }
   };
 
@@ -274,45 +289,76 @@ __global__ void __launch_bounds__(WM * WN * 64) k_linear_tile(LinearArgs a) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
-  const int fr = lane & 31, fq = lane >> 5;
-  if (steps > 0) fetch(0, 0);
-  for (int s = 0; s < steps; ++s) {
-    const int buf = s & 1;
-    if constexpr (DMA) {
-      wait_vmcnt<0>();  // this wave's part of the K-tile is in LDS
-      wg_barrier();     // every wave's is, and the other buffer is free
-      if (s + 1 < steps) fetch(s + 1, buf ^ 1);
-    } else {
-      store(buf);
-      __syncthreads();
-      if (s + 1 < steps) fetch(s + 1, buf ^ 1);
-    }
-    const char* A = lds[buf] + (wm * FM * 32 + fr) * ROW;
-    const char* B = lds[buf] + BM * ROW + (wn * FN * 32 + fr) * ROW;
+  const int fr = lane & 31, fq = lane >> 5, sw = swz(fr);
+  const char* const A = lds + (wm * FM * 32 + fr) * ROW;
+  const char* const B = lds + (BM + wn * FN * 32 + fr) * ROW;
+  u32x4 xf[2][FM], wf[2][FN];
+  auto read = [&](int buf, int ks, int set) {
+    const int c = buf * BUF + (((ks * 2 + fq) ^ sw) << 4);
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) {
-      const int c = ((ks * 2 + fq) ^ swz(fr)) << 4;
-      u32x4 xf[FM], wf[FN];
+    for (int i = 0; i < FM; ++i) xf[set][i] = *reinterpret_cast<const u32x4*>(A + i * 32 * ROW + c);
 #pragma unroll
-      for (int i = 0; i < FM; ++i) xf[i] = *reinterpret_cast<const u32x4*>(A + i * 32 * ROW + c);
+    for (int j = 0; j < FN; ++j) wf[set][j] = *reinterpret_cast<const u32x4*>(B + j * 32 * ROW + c);
+  };
+  auto mma = [&](int set) {
 #pragma unroll
-      for (int j = 0; j < FN; ++j) wf[j] = *reinterpret_cast<const u32x4*>(B + j * 32 * ROW + c);
+    for (int i = 0; i < FM; ++i)
 #pragma unroll
-      for (int i = 0; i < FM; ++i)
+      for (int j = 0; j < FN; ++j) acc[i][j] = L::mma32(wf[set][j], xf[set][i], acc[i][j]);
+  };
+
+  if (steps > 0) {
+    fetch(0, 0);
+    store(0);
+    if constexpr (DMA) wait_vmcnt<0>();
+    wait_lgkm0();
+    wg_barrier();
+    if (DMA && steps > 1) fetch(1, 1);
+    read(0, 0, 0);
+    for (int s = 0; s < steps; ++s) {
+      const int buf = s & 1;
+      const bool more = s + 1 < steps;
+      if (!DMA && more) fetch(s + 1, buf ^ 1);
 #pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = L::mma32(wf[j], xf[i], acc[i][j]);
+      for (int ks = 0; ks < 3; ++ks) {
+        read(buf, ks + 1, (ks + 1) & 1);
+        __builtin_amdgcn_sched_barrier(0);  // the reads are under way before the MFMAs
+        mma(ks & 1);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (more) {
+        store(buf ^ 1);
+        if constexpr (DMA) wait_vmcnt<0>();  // this wave's part of the next K-tile is in LDS
+        __asm__ __volatile__("" ::: "memory");
+        wait_lgkm0();  // and its last operands of this one are in registers
+        wg_barrier();  // so are every wave's
+        if (DMA && s + 2 < steps) fetch(s + 2, buf);
+        read(buf ^ 1, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      mma(1);
     }
   }
 
-  // block (i, j): lane l holds row l % 32 and features 8 g + 4 (l / 32) .. of g = 0 .. 3
+  // The finished tile through LDS, a block of 32 rows per wave row at a time, so that
+  // whole rows are written.  Block (i, j): lane l holds row l % 32 and
+  // features 8 g + 4 (l / 32) .. of g = 0 .. 3.
+  float* const out = reinterpret_cast<float*>(lds);
 #pragma unroll
-  for (int i = 0; i < FM; ++i)
+  for (int i = 0; i < FM; ++i) {
+    __syncthreads();
 #pragma unroll
     for (int j = 0; j < FN; ++j)
 #pragma unroll
       for (int g = 0; g < 4; ++g)
-        finish4(a, m0 + (wm * FM + i) * 32 + fr, n0 + (wn * FN + j) * 32 + 8 * g + 4 * fq,
-                floatx4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]});
+        *reinterpret_cast<floatx4*>(out + (wm * 32 + fr) * PITCH + (wn * FN + j) * 32 + 8 * g + 4 * fq) =
+            floatx4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+    __syncthreads();
+    for (int t = tid; t < WM * 32 * (BN / 4); t += NT) {
+      const int r = t / (BN / 4), n = t % (BN / 4) * 4;
+      finish4(a, m0 + (r / 32 * FM + i) * 32 + r % 32, n0 + n, *reinterpret_cast<const floatx4*>(out + r * PITCH + n));
+    }
+  }
 }
 
 template <class T, int FM, int FN, int NW, int U>
