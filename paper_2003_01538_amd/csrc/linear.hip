@@ -76,49 +76,66 @@ __device__ __forceinline__ float activate(float v, int act) {
   return v;
 }
 
-// bias, residual, activation and the one rounding of outputs (m, n .. n + 3),
-// those that exist
-__device__ __forceinline__ void finish4(const LinearArgs& a, int m, int n, floatx4 v) {
-  if (m >= a.M || n >= a.N) return;
-  const int64_t o = (int64_t)m * a.ldy + n, ro = (int64_t)m * a.ldres + n;
+// The bias of features n .. n + 3, 0 for those that do not exist.
+struct Bias4 {
+  floatx4 v = {0.f, 0.f, 0.f, 0.f};
+  __device__ __forceinline__ Bias4(const LinearArgs& a, int n) {
+    if (!a.bias) return;
+    if (n + 4 <= a.N) {
+      v = *reinterpret_cast<const floatx4_at4*>(a.bias + n);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (n + e < a.N) v[e] = a.bias[n + e];
+    }
+  }
+};
+
+// The residual of outputs (m, n .. n + 3), 0 for those that do not exist.
+__device__ __forceinline__ floatx4 residual4(const LinearArgs& a, int m, int n) {
+  floatx4 r = {0.f, 0.f, 0.f, 0.f};
+  if (!a.res || m >= a.M) return r;
+  const int64_t o = (int64_t)m * a.ldres + n;
+  const float* const f = static_cast<const float*>(a.res) + o;
+  const uint16_t* const h = static_cast<const uint16_t*>(a.res) + o;
   if (n + 4 <= a.N) {
-    if (a.bias) {
-      const floatx4 b = *reinterpret_cast<const floatx4_at4*>(a.bias + n);
-      v += b;
-    }
-    floatx4 r = {0.f, 0.f, 0.f, 0.f};
-    if (a.res) {
-      if (a.out_f32) {
-        r = *reinterpret_cast<const floatx4_at4*>(static_cast<const float*>(a.res) + ro);
-      } else {
-        const u32x2 q = *reinterpret_cast<const u32x2_at2*>(static_cast<const uint16_t*>(a.res) + ro);
-        r = floatx4{__uint_as_float(q[0] << 16), __uint_as_float(q[0] & 0xffff0000u), __uint_as_float(q[1] << 16),
-                    __uint_as_float(q[1] & 0xffff0000u)};
-      }
-      if (a.res_first) v += r;
-    }
+    if (a.out_f32) return *reinterpret_cast<const floatx4_at4*>(f);
+    const u32x2 q = *reinterpret_cast<const u32x2_at2*>(h);
+    return floatx4{__uint_as_float(q[0] << 16), __uint_as_float(q[0] & 0xffff0000u), __uint_as_float(q[1] << 16),
+                   __uint_as_float(q[1] & 0xffff0000u)};
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (n + e < a.N) r[e] = a.out_f32 ? f[e] : bf2f(h[e]);
+  return r;
+}
+
+// Bias, residual, activation and the one rounding of those of outputs
+// (m, n .. n + 3) that exist.
+__device__ __forceinline__ void finish4(const LinearArgs& a, int m, int n, floatx4 v, const Bias4& bias, floatx4 res) {
+  if (m >= a.M || n >= a.N) return;
+  v += bias.v;
+  if (a.res_first) v += res;
+  if (a.act != FS_ACT_NONE) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = activate(v[e], a.act);
-    if (a.res && !a.res_first) v += r;
-    if (a.out_f32) {
-      *reinterpret_cast<floatx4_at4*>(static_cast<float*>(a.y) + o) = v;
-    } else {
-      *reinterpret_cast<u32x2_at2*>(static_cast<uint16_t*>(a.y) + o) =
-          u32x2{f2bf(v[0]) | uint32_t(f2bf(v[1])) << 16, f2bf(v[2]) | uint32_t(f2bf(v[3])) << 16};
-    }
+  }
+  if (a.res && !a.res_first) v += res;
+  const int64_t o = (int64_t)m * a.ldy + n;
+  float* const f = static_cast<float*>(a.y) + o;
+  uint16_t* const h = static_cast<uint16_t*>(a.y) + o;
+  if (n + 4 <= a.N) {
+    if (a.out_f32) *reinterpret_cast<floatx4_at4*>(f) = v;
+    else
+      *reinterpret_cast<u32x2_at2*>(h) = u32x2{f2bf(v[0]) | uint32_t(f2bf(v[1])) << 16, f2bf(v[2]) | uint32_t(f2bf(v[3])) << 16};
     return;
   }
-  for (int e = 0; n + e < a.N; ++e) {
-    float s = v[e];
-    if (a.bias) s += a.bias[n + e];
-    float r = 0.f;
-    if (a.res) r = a.out_f32 ? static_cast<const float*>(a.res)[ro + e] : bf2f(static_cast<const uint16_t*>(a.res)[ro + e]);
-    if (a.res && a.res_first) s += r;
-    s = activate(s, a.act);
-    if (a.res && !a.res_first) s += r;
-    if (a.out_f32) static_cast<float*>(a.y)[o + e] = s;
-    else static_cast<uint16_t*>(a.y)[o + e] = f2bf(s);
-  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (n + e < a.N) {
+      if (a.out_f32) f[e] = v[e];
+      else h[e] = f2bf(v[e]);
+    }
 }
 
 // --------------------------------------------------------------- few tiles
@@ -202,7 +219,8 @@ __global__ void __launch_bounds__(NW * 64) k_linear_few(LinearArgs a) {
     floatx4 s = part[0][b][l];
 #pragma unroll
     for (int q = 1; q < NW; ++q) s += part[q][b][l];
-    finish4(a, m0 + b / FN * 16 + (l & 15), n0 + b % FN * 16 + (l >> 4) * 4, s);
+    const int m = m0 + b / FN * 16 + (l & 15), n = n0 + b % FN * 16 + (l >> 4) * 4;
+    finish4(a, m, n, s, Bias4(a, n), residual4(a, m, n));
   }
 }
 
@@ -342,21 +360,34 @@ __global__ void __launch_bounds__(WM * WN * 64) k_linear_tile(LinearArgs a) {
 
   // The finished tile through LDS, a block of 32 rows per wave row at a time, so that
   // whole rows are written.  Block (i, j): lane l holds row l % 32 and
-  // features 8 g + 4 (l / 32) .. of g = 0 .. 3.
+  // features 8 g + 4 (l / 32) .. of g = 0 .. 3.  On the way out a thread keeps its 4
+  // features and walks the rows; the residuals of the rows to come are on their way.
   float* const out = reinterpret_cast<float*>(lds);
-#pragma unroll
+  constexpr int TR = NT / (BN / 4), PASSES = WM * 32 / TR;  // rows per pass
+  const int n = n0 + tid % (BN / 4) * 4, r0 = tid / (BN / 4);
+  const Bias4 bias(a, n);
   for (int i = 0; i < FM; ++i) {
+    auto row = [&](int pass) {
+      const int r = pass * TR + r0;
+      return m0 + (r / 32 * FM + i) * 32 + r % 32;
+    };
+    floatx4 res = residual4(a, row(0), n);
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < FN; ++j)
+    for (int ii = 0; ii < FM; ++ii)
+      if (ii == i)
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<floatx4*>(out + (wm * 32 + fr) * PITCH + (wn * FN + j) * 32 + 8 * g + 4 * fq) =
-            floatx4{acc[i][j][4 * g], acc[i][j][4 * g + 1], acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]};
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+          for (int g = 0; g < 4; ++g)
+            *reinterpret_cast<floatx4*>(out + (wm * 32 + fr) * PITCH + (wn * FN + j) * 32 + 8 * g + 4 * fq) =
+                floatx4{acc[ii][j][4 * g], acc[ii][j][4 * g + 1], acc[ii][j][4 * g + 2], acc[ii][j][4 * g + 3]};
     __syncthreads();
-    for (int t = tid; t < WM * 32 * (BN / 4); t += NT) {
-      const int r = t / (BN / 4), n = t % (BN / 4) * 4;
-      finish4(a, m0 + (r / 32 * FM + i) * 32 + r % 32, n0 + n, *reinterpret_cast<const floatx4*>(out + r * PITCH + n));
+#pragma unroll 2
+    for (int pass = 0; pass < PASSES; ++pass) {
+      const floatx4 now = res;
+      if (pass + 1 < PASSES) res = residual4(a, row(pass + 1), n);
+      finish4(a, row(pass), n, *reinterpret_cast<const floatx4*>(out + (pass * TR + r0) * PITCH + n - n0), bias, now);
     }
   }
 }
