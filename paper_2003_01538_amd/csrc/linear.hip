@@ -228,11 +228,6 @@ __global__ void __launch_bounds__(NW * 64) k_linear_few(LinearArgs a) {
 // A tile of BM rows x BN features on WM x WN waves.  K-tiles of 128 bytes a row
 // lie in LDS as in lds_dma.hpp, two of them in turn.  DMA: the loads write LDS
 // themselves (rows aligned to 16 bytes); otherwise they pass through registers.
-//
-// A K-tile is four steps of MFMAs.  The operands of a step are read from LDS during
-// the step before it; the barrier between two K-tiles lies before the last step,
-// whose operands are in registers by then, so the matrix cores have work while
-// the waves meet and the next K-tile's first operands are read.
 template <class T, int BM, int BN, int WM, int WN, bool DMA>
 __global__ void __launch_bounds__(WM * WN * 64) k_linear_tile(LinearArgs a) {
   using L = LinT<T>;
@@ -273,12 +268,13 @@ __global__ void __launch_bounds__(WM * WN * 64) k_linear_tile(LinearArgs a) {
       off[p] = ok ? (uint32_t)((r * (p < PA ? a.ldx : a.ldw) + kc) * ES) : OOB;  // stays out of range with any k added
     }
   }
-  auto fetch = [&](int s, int buf) {
+  auto fetch = [&](int s, int buf, uint32_t set = ~0u) {  // pieces p of which bit p is set
     const int k0 = s * KT;
     if constexpr (DMA) {
-      const uint32_t kb = k0 + kc < a.K ? (uint32_t)(k0 * ES) : OOB;
+      const uint32_t kb = k0 + kc < a.K ? (uint32_t)(k0 * ES) : OOB;  // behind the end: zeros, in the same number of loads
 #pragma unroll
       for (int p = 0; p < PA + PB; ++p) {
+        if (!(set >> p & 1)) continue;
         char* to = lds + buf * BUF + (p * NT + wave * 64) * 16;
         const uint32_t o = max(off[p], kb) == OOB ? OOB : off[p] + kb;
         __builtin_amdgcn_raw_ptr_buffer_load_lds(p < PA ? rx : rw, (lds_void*)to, 16, o, 0, 0, 0);
@@ -310,27 +306,104 @@ __global__ void __launch_bounds__(WM * WN * 64) k_linear_tile(LinearArgs a) {
   const int fr = lane & 31, fq = lane >> 5, sw = swz(fr);
   const char* const A = lds + (wm * FM * 32 + fr) * ROW;
   const char* const B = lds + (BM + wn * FN * 32 + fr) * ROW;
-  u32x4 xf[2][FM], wf[2][FN];
-  auto read = [&](int buf, int ks, int set) {
-    const int c = buf * BUF + (((ks * 2 + fq) ^ sw) << 4);
-#pragma unroll
-    for (int i = 0; i < FM; ++i) xf[set][i] = *reinterpret_cast<const u32x4*>(A + i * 32 * ROW + c);
-#pragma unroll
-    for (int j = 0; j < FN; ++j) wf[set][j] = *reinterpret_cast<const u32x4*>(B + j * 32 * ROW + c);
+  auto operand = [&](const char* base, int buf, int ks, int block) {
+    return *reinterpret_cast<const u32x4*>(base + block * 32 * ROW + buf * BUF + (((ks * 2 + fq) ^ sw) << 4));
   };
-  auto mma = [&](int set) {
-#pragma unroll
-    for (int i = 0; i < FM; ++i)
-#pragma unroll
-      for (int j = 0; j < FN; ++j) acc[i][j] = L::mma32(wf[set][j], xf[set][i], acc[i][j]);
+  auto meet = [&] {
+    __asm__ __volatile__("" ::: "memory");
+    wait_lgkm0();  // the operands read last are in registers
+    wg_barrier();
   };
 
-  if (steps > 0) {
+  if constexpr (DMA && FM % 2 == 0) {
+    // Two halves per K-tile, of the upper and the lower half of the wave's row blocks.
+    // The first runs on x0 and w, the second on x1 and w; during the first x1 is
+    // read, during the second the next K-tile's x0 and w (a step's w once its MFMAs
+    // have it).  So LDS is free for the K-tile after the next early, x0 and w when
+    // the first half begins, x1 when the second does, and every load has one and a
+    // half K-tiles of time.  A half waits for the loads whose operands are read in
+    // it: all but the eight issued last.
+    constexpr int H = FM / 2, PH = H * 32 / (NT / 8);  // pieces of a half of a wave row's blocks
+    static_assert(H * 32 % (NT / 8) == 0 && PA == 2 * WM * PH, "pieces and halves");
+    constexpr uint32_t LOW = [] {
+      uint32_t set = 0;
+      for (int p = 0; p < PA; ++p) set |= (p / PH % 2 == 1 ? 1u : 0u) << p;
+      return set;
+    }();
+    constexpr uint32_t UP = ~LOW;
+    constexpr int N_LOW = PA / 2, N_ALL = PA + PB;
+    u32x4 x0[4][H], x1[4][H], w[4][FN];
+    fetch(0, 0, UP);
+    fetch(0, 0, LOW);
+    fetch(1, 1, UP);
+    fetch(1, 1, LOW);
+    wait_vmcnt<N_LOW + N_ALL>();
+    wg_barrier();
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+#pragma unroll
+      for (int i = 0; i < H; ++i) x0[ks][i] = operand(A, 0, ks, i);
+#pragma unroll
+      for (int j = 0; j < FN; ++j) w[ks][j] = operand(B, 0, ks, j);
+    }
+    for (int s = 0; s < steps; ++s) {
+      const int buf = s & 1;
+      wait_vmcnt<N_ALL>();
+      meet();
+      fetch(s + 2, buf, UP);
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+        for (int i = 0; i < H; ++i) x1[ks][i] = operand(A, buf, ks, H + i);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+        for (int i = 0; i < H; ++i)
+#pragma unroll
+          for (int j = 0; j < FN; ++j) acc[i][j] = L::mma32(w[ks][j], x0[ks][i], acc[i][j]);
+      __builtin_amdgcn_sched_barrier(0);
+      wait_vmcnt<N_ALL>();
+      meet();
+      fetch(s + 2, buf, LOW);
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+        for (int i = 0; i < H; ++i) x0[ks][i] = operand(A, buf ^ 1, ks, i);
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) {
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < H; ++i)
+#pragma unroll
+          for (int j = 0; j < FN; ++j) acc[H + i][j] = L::mma32(w[ks][j], x1[ks][i], acc[H + i][j]);
+#pragma unroll
+        for (int j = 0; j < FN; ++j) w[ks][j] = operand(B, buf ^ 1, ks, j);
+      }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+    wait_vmcnt<0>();
+    meet();
+  } else if (steps > 0) {
+    // A step's operands are read during the step before it; the barrier between two
+    // K-tiles lies before the last step, whose operands are in registers by then.
+    u32x4 xf[2][FM], wf[2][FN];
+    auto read = [&](int buf, int ks, int set) {
+#pragma unroll
+      for (int i = 0; i < FM; ++i) xf[set][i] = operand(A, buf, ks, i);
+#pragma unroll
+      for (int j = 0; j < FN; ++j) wf[set][j] = operand(B, buf, ks, j);
+    };
+    auto mma = [&](int set) {
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = L::mma32(wf[set][j], xf[set][i], acc[i][j]);
+    };
     fetch(0, 0);
     store(0);
     if constexpr (DMA) wait_vmcnt<0>();
-    wait_lgkm0();
-    wg_barrier();
+    meet();
     if (DMA && steps > 1) fetch(1, 1);
     read(0, 0, 0);
     for (int s = 0; s < steps; ++s) {
@@ -347,9 +420,7 @@ __global__ void __launch_bounds__(WM * WN * 64) k_linear_tile(LinearArgs a) {
       if (more) {
         store(buf ^ 1);
         if constexpr (DMA) wait_vmcnt<0>();  // this wave's part of the next K-tile is in LDS
-        __asm__ __volatile__("" ::: "memory");
-        wait_lgkm0();  // and its last operands of this one are in registers
-        wg_barrier();  // so are every wave's
+        meet();                              // every wave's is, and all are done with this one
         if (DMA && s + 2 < steps) fetch(s + 2, buf);
         read(buf ^ 1, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
