@@ -69,6 +69,11 @@ __device__ __forceinline__ u32x4 piece(const T* row, int k, int K) {
   return __builtin_bit_cast(u32x4, t);
 }
 
+// 64 lanes' 16 bytes at their offsets to LDS, in lane order.
+__device__ __forceinline__ void load_lds(__amdgpu_buffer_rsrc_t r, char* to, uint32_t off) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)to, 16, off, 0, 0, 0);
+}
+
 __device__ __forceinline__ float activate(float v, int act) {
   if (act == FS_ACT_RELU) return v > 0.f ? v : 0.f;
   if (act == FS_ACT_GELU) return 0.5f * v * (1.f + erff(v * 0.70710678f));
@@ -263,22 +268,23 @@ __global__ void __launch_bounds__(WM * WN * 64) k_linear_tile(LinearArgs a) {
   if constexpr (DMA) {
 #pragma unroll
     for (int p = 0; p < PA + PB; ++p) {
-      const int r = prow + (p < PA ? p : p - PA) * (NT / 8);
-      const bool ok = p < PA ? m0 + r < a.M : n0 + r < a.N;
-      off[p] = ok ? (uint32_t)((r * (p < PA ? a.ldx : a.ldw) + kc) * ES) : OOB;  // stays out of range with any k added
+      // rows that do not exist read the last one: they enter only outputs that do not exist
+      const int r = prow + (p < PA ? p : p - PA) * (NT / 8), last = (p < PA ? a.M - m0 : a.N - n0) - 1;
+      off[p] = (uint32_t)((min(r, last) * (p < PA ? a.ldx : a.ldw) + kc) * ES);
     }
   }
-  auto fetch = [&](int s, int buf, uint32_t set = ~0u) {  // pieces p of which bit p is set
+  // the offset of K-tile s; behind the reduction's end out of range: zeros, by the same number of loads
+  auto tile_off = [&](int s) { return s * KT + kc < a.K ? (uint32_t)(s * KT * ES) : OOB; };
+  auto fetch_piece = [&](auto p, uint32_t kb, int buf) {
+    if constexpr (DMA) {
+      load_lds(p < PA ? rx : rw, lds + buf * BUF + (p * NT + wave * 64) * 16, off[p] + kb);
+    }
+  };
+  auto fetch = [&](int s, int buf) {
     const int k0 = s * KT;
     if constexpr (DMA) {
-      const uint32_t kb = k0 + kc < a.K ? (uint32_t)(k0 * ES) : OOB;  // behind the end: zeros, in the same number of loads
-#pragma unroll
-      for (int p = 0; p < PA + PB; ++p) {
-        if (!(set >> p & 1)) continue;
-        char* to = lds + buf * BUF + (p * NT + wave * 64) * 16;
-        const uint32_t o = max(off[p], kb) == OOB ? OOB : off[p] + kb;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(p < PA ? rx : rw, (lds_void*)to, 16, o, 0, 0, 0);
-      }
+      const uint32_t kb = tile_off(s);
+      static_for<0, PA + PB>([&](auto p) { fetch_piece(p, kb, buf); });
     } else {
 #pragma unroll
       for (int p = 0; p < PA + PB; ++p) {
@@ -320,23 +326,39 @@ __global__ void __launch_bounds__(WM * WN * 64) k_linear_tile(LinearArgs a) {
     // The first runs on x0 and w, the second on x1 and w; during the first x1 is
     // read, during the second the next K-tile's x0 and w (a step's w once its MFMAs
     // have it).  So LDS is free for the K-tile after the next early, x0 and w when
-    // the first half begins, x1 when the second does, and every load has one and a
-    // half K-tiles of time.  A half waits for the loads whose operands are read in
-    // it: all but the eight issued last.
-    constexpr int H = FM / 2, PH = H * 32 / (NT / 8);  // pieces of a half of a wave row's blocks
+    // the first half begins, x1 when the second does, and every load has about one
+    // and a half K-tiles of time.  A half waits for the loads whose operands are read
+    // in it, all but the N_ALL issued last, after its first step, whose operands are in
+    // registers by then.  Reads and loads are issued between MFMAs, in their shadow.
+    constexpr int H = FM / 2, PH = H * 32 / (NT / 8);  // row blocks of a half; its pieces per wave row
     static_assert(H * 32 % (NT / 8) == 0 && PA == 2 * WM * PH, "pieces and halves");
-    constexpr uint32_t LOW = [] {
-      uint32_t set = 0;
-      for (int p = 0; p < PA; ++p) set |= (p / PH % 2 == 1 ? 1u : 0u) << p;
-      return set;
-    }();
-    constexpr uint32_t UP = ~LOW;
-    constexpr int N_LOW = PA / 2, N_ALL = PA + PB;
+    constexpr int N_LOW = PA / 2, N_UP = PA / 2 + PB, N_ALL = PA + PB;
     u32x4 x0[4][H], x1[4][H], w[4][FN];
-    fetch(0, 0, UP);
-    fetch(0, 0, LOW);
-    fetch(1, 1, UP);
-    fetch(1, 1, LOW);
+    // the n-th piece of the lower half's rows, of the upper half's and w
+    auto low = [&](auto n, uint32_t kb, int buf) {
+      fetch_piece(std::integral_constant<int, (n / PH * 2 + 1) * PH + n % PH>{}, kb, buf);
+    };
+    auto up = [&](auto n, uint32_t kb, int buf) {
+      if constexpr (n < PA / 2) fetch_piece(std::integral_constant<int, n / PH * 2 * PH + n % PH>{}, kb, buf);
+      else fetch_piece(std::integral_constant<int, PA / 2 + n>{}, kb, buf);
+    };
+    // the MFMAs of a step on rows of block base + i, and the L items that fall between them
+    auto step = [&](auto base, const u32x4 (&x)[H], const u32x4 (&v)[FN], auto L_items, auto&& item) {
+      constexpr int Q = H * FN, LI = L_items;
+      static_for<0, Q>([&](auto q) {
+        acc[base + q / FN][q % FN] = L::mma32(v[q % FN], x[q / FN], acc[base + q / FN][q % FN]);
+        static_for<(q * LI + Q - 1) / Q, ((q + 1) * LI + Q - 1) / Q>([&](auto n) { item(n); });
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    };
+    constexpr std::integral_constant<int, 0> first{};
+    constexpr std::integral_constant<int, H> second{};
+    auto none = [](auto) {};
+    for (int t = 0; t < 2; ++t) {
+      const uint32_t kb = tile_off(t);
+      static_for<0, N_UP>([&](auto n) { up(n, kb, t); });
+      static_for<0, N_LOW>([&](auto n) { low(n, kb, t); });
+    }
     wait_vmcnt<N_LOW + N_ALL>();
     wg_barrier();
 #pragma unroll
@@ -348,39 +370,38 @@ __global__ void __launch_bounds__(WM * WN * 64) k_linear_tile(LinearArgs a) {
     }
     for (int s = 0; s < steps; ++s) {
       const int buf = s & 1;
+      const uint32_t kb = tile_off(s + 2);
+      constexpr int U1 = (N_UP + 2) / 3, U2 = (N_UP - U1 + 1) / 2, U3 = N_UP - U1 - U2;
+      __builtin_amdgcn_sched_barrier(0);
+      step(first, x0[0], w[0], std::integral_constant<int, 0>{}, none);
       wait_vmcnt<N_ALL>();
       meet();
-      fetch(s + 2, buf, UP);
-#pragma unroll
-      for (int ks = 0; ks < 4; ++ks)
-#pragma unroll
-        for (int i = 0; i < H; ++i) x1[ks][i] = operand(A, buf, ks, H + i);
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int ks = 0; ks < 4; ++ks)
-#pragma unroll
-        for (int i = 0; i < H; ++i)
-#pragma unroll
-          for (int j = 0; j < FN; ++j) acc[i][j] = L::mma32(w[ks][j], x0[ks][i], acc[i][j]);
-      __builtin_amdgcn_sched_barrier(0);
+      auto read_x1 = [&](auto n) { x1[n / H][n % H] = operand(A, buf, n / H, H + n % H); };
+      step(first, x0[1], w[1], std::integral_constant<int, 2 * H + U1>{}, [&](auto n) {
+        if constexpr (n < 2 * H) read_x1(n);
+        else up(std::integral_constant<int, n - 2 * H>{}, kb, buf);
+      });
+      step(first, x0[2], w[2], std::integral_constant<int, 2 * H + U2>{}, [&](auto n) {
+        if constexpr (n < 2 * H) read_x1(std::integral_constant<int, 2 * H + n>{});
+        else up(std::integral_constant<int, n - 2 * H + U1>{}, kb, buf);
+      });
+      step(first, x0[3], w[3], std::integral_constant<int, U3>{}, [&](auto n) { up(std::integral_constant<int, n + U1 + U2>{}, kb, buf); });
+      step(second, x1[0], w[0], std::integral_constant<int, 0>{}, none);
       wait_vmcnt<N_ALL>();
       meet();
-      fetch(s + 2, buf, LOW);
-#pragma unroll
-      for (int ks = 0; ks < 4; ++ks)
-#pragma unroll
-        for (int i = 0; i < H; ++i) x0[ks][i] = operand(A, buf ^ 1, ks, i);
-#pragma unroll
-      for (int ks = 0; ks < 4; ++ks) {
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int i = 0; i < H; ++i)
-#pragma unroll
-          for (int j = 0; j < FN; ++j) acc[H + i][j] = L::mma32(w[ks][j], x1[ks][i], acc[H + i][j]);
-#pragma unroll
-        for (int j = 0; j < FN; ++j) w[ks][j] = operand(B, buf ^ 1, ks, j);
-      }
-      __builtin_amdgcn_sched_barrier(0);
+      auto read_x0 = [&](auto n) { x0[n / H][n % H] = operand(A, buf ^ 1, n / H, n % H); };
+      auto read_w = [&](auto ks, auto n) { w[ks][n] = operand(B, buf ^ 1, ks, n); };
+      step(second, x1[1], w[1], std::integral_constant<int, 2 * H + FN + N_LOW>{}, [&](auto n) {
+        if constexpr (n < 2 * H) read_x0(n);
+        else if constexpr (n < 2 * H + FN) read_w(std::integral_constant<int, 0>{}, std::integral_constant<int, n - 2 * H>{});
+        else low(std::integral_constant<int, n - 2 * H - FN>{}, kb, buf);
+      });
+      step(second, x1[2], w[2], std::integral_constant<int, 2 * H + FN>{}, [&](auto n) {
+        if constexpr (n < 2 * H) read_x0(std::integral_constant<int, 2 * H + n>{});
+        else read_w(std::integral_constant<int, 1>{}, std::integral_constant<int, n - 2 * H>{});
+      });
+      step(second, x1[3], w[3], std::integral_constant<int, FN>{}, [&](auto n) { read_w(std::integral_constant<int, 2>{}, n); });
+      static_for<0, FN>([&](auto n) { read_w(std::integral_constant<int, 3>{}, n); });
     }
     wait_vmcnt<0>();
     meet();
