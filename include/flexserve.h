@@ -437,7 +437,7 @@ fs_status fs_conv_bf16_device_noalloc(const void *d_in, int32_t B, int32_t H, in
  *  - every tensor pointer is a device pointer of the current device (a
  *    tensor of another device, or host memory, is FS_ERR_INVALID), aligned to
  *    its elements; rows lie `ld` elements apart (ld >= the row's length, need
- *    not be a multiple of anything).  Sizes and offsets are 64-bit inside.
+ *    not be a multiple of anything; beyond 2^40 FS_ERR_UNSUPPORTED).  Sizes and offsets are 64-bit inside.
  *  - the call is asynchronous on `stream` (a hipStream_t of the current
  *    device, NULL = the null stream); it allocates nothing, copies nothing to
  *    or from the host and may be captured into a graph.

@@ -57,16 +57,37 @@ template <> struct LinT<float> {
   }
 };
 
-// 16 bytes of a row at any element (the hardware takes vector accesses at every
-// byte address); zeros behind its end.
+// 16 bytes of a row at any element: the hardware takes vector accesses at every
+// byte address.
+template <class T>
+__device__ __forceinline__ u32x4 full_piece(const T* row, int k) {
+  return *reinterpret_cast<const u32x4_at2*>(row + k);
+}
+
+// The same with zeros behind the row's end: the last 16 bytes of the row, shifted.
 template <class T>
 __device__ __forceinline__ u32x4 piece(const T* row, int k, int K) {
   constexpr int VEC = LinT<T>::VEC;
-  if (k + VEC <= K) return *reinterpret_cast<const u32x4_at2*>(row + k);
-  T t[VEC];
+  if (K < VEC) {  // no 16 bytes to load
+    T t[VEC];
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) t[e] = k + e < K ? row[k + e] : T(0);
-  return __builtin_bit_cast(u32x4, t);
+    for (int e = 0; e < VEC; ++e) t[e] = k + e < K ? row[k + e] : T(0);
+    return __builtin_bit_cast(u32x4, t);
+  }
+  const int from = min(k, K - VEC), bits = min(k - from, VEC) * (int)sizeof(T) * 8;
+  const u32x4 v = full_piece(row, from);
+  const uint64_t lo = v[0] | uint64_t(v[1]) << 32, hi = v[2] | uint64_t(v[3]) << 32;
+  uint64_t l = lo, h = hi;
+  if (bits >= 128) {
+    l = h = 0;
+  } else if (bits >= 64) {
+    l = hi >> (bits - 64);
+    h = 0;
+  } else if (bits > 0) {
+    l = lo >> bits | hi << (64 - bits);
+    h = hi >> bits;
+  }
+  return u32x4{uint32_t(l), uint32_t(l >> 32), uint32_t(h), uint32_t(h >> 32)};
 }
 
 // 64 lanes' 16 bytes at their offsets to LDS, in lane order.
@@ -178,6 +199,14 @@ __global__ void __launch_bounds__(NW * 64) k_linear_few(LinearArgs a) {
     const int m = m0 + i * 16 + (lane & 15);
     xr[i] = static_cast<const T*>(a.x) + (int64_t)(m < a.M ? m : 0) * a.ldx;
   }
+  // the outputs that this thread finishes: block (i, j) of 16 x 16, in which lane l
+  // holds row l % 16 and features 4 (l / 16) ..
+  static_assert(FM * FN <= NW, "a block per wave");
+  const int om = m0 + wave / FN * 16 + (lane & 15), on = n0 + wave % FN * 16 + (lane >> 4) * 4;
+  const bool finishes = wave < FM * FN;
+  const Bias4 bias(a, finishes ? on : a.N);
+  const floatx4 res = residual4(a, finishes ? om : a.M, on);
+
   floatx4 acc[FM][FN];
 #pragma unroll
   for (int i = 0; i < FM; ++i)
@@ -201,9 +230,9 @@ __global__ void __launch_bounds__(NW * 64) k_linear_few(LinearArgs a) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
 #pragma unroll
-        for (int j = 0; j < FN; ++j) w[u][j][h] = *reinterpret_cast<const u32x4_at2*>(wr[j] + ku + h * VEC);
+        for (int j = 0; j < FN; ++j) w[u][j][h] = full_piece(wr[j], ku + h * VEC);
 #pragma unroll
-        for (int i = 0; i < FM; ++i) x[u][i][h] = *reinterpret_cast<const u32x4_at2*>(xr[i] + ku + h * VEC);
+        for (int i = 0; i < FM; ++i) x[u][i][h] = full_piece(xr[i], ku + h * VEC);
       }
     }
     __builtin_amdgcn_sched_barrier(0);  // all loads are under way before the first product waits
@@ -226,15 +255,11 @@ __global__ void __launch_bounds__(NW * 64) k_linear_few(LinearArgs a) {
 #pragma unroll
     for (int j = 0; j < FN; ++j) part[wave][i * FN + j][lane] = acc[i][j];
   __syncthreads();
-  // block (i, j): lane l holds row l % 16 and features 4 (l / 16) ..
-  for (int t = tid; t < FM * FN * 64; t += NW * 64) {
-    const int b = t >> 6, l = t & 63;
-    floatx4 s = part[0][b][l];
+  if (!finishes) return;
+  floatx4 s = part[0][wave][lane];
 #pragma unroll
-    for (int q = 1; q < NW; ++q) s += part[q][b][l];
-    const int m = m0 + b / FN * 16 + (l & 15), n = n0 + b % FN * 16 + (l >> 4) * 4;
-    finish4(a, m, n, s, Bias4(a, n), residual4(a, m, n));
-  }
+  for (int q = 1; q < NW; ++q) s += part[q][wave][lane];
+  finish4(a, om, on, s, bias, res);
 }
 
 // -------------------------------------------------------------- many tiles
@@ -271,15 +296,13 @@ __global__ void __launch_bounds__(WM * WN * 64) k_linear_tile(LinearArgs a) {
   const int prow = tid >> 3, kc = ((tid & 7) ^ swz(prow)) * VEC;
   const __amdgpu_buffer_rsrc_t rx = rsrc(xb, DMA ? (uint32_t)(((min(BM, a.M - m0) - 1) * a.ldx + a.K) * ES) : 0u);
   const __amdgpu_buffer_rsrc_t rw = rsrc(wb, DMA ? (uint32_t)(((min(BN, a.N - n0) - 1) * a.ldw + a.K) * ES) : 0u);
-  uint32_t off[DMA ? PA + PB : 1];
+  uint32_t off[PA + PB];  // bytes from the tile's first row
   u32x4 reg[DMA ? 1 : PA + PB];
-  if constexpr (DMA) {
 #pragma unroll
-    for (int p = 0; p < PA + PB; ++p) {
-      // rows that do not exist read the last one: they enter only outputs that do not exist
-      const int r = prow + (p < PA ? p : p - PA) * (NT / 8), last = (p < PA ? a.M - m0 : a.N - n0) - 1;
-      off[p] = (uint32_t)((min(r, last) * (p < PA ? a.ldx : a.ldw) + kc) * ES);
-    }
+  for (int p = 0; p < PA + PB; ++p) {
+    // rows that do not exist read the last one: they enter only outputs that do not exist
+    const int r = prow + (p < PA ? p : p - PA) * (NT / 8), last = (p < PA ? a.M - m0 : a.N - n0) - 1;
+    off[p] = (uint32_t)((min(r, last) * (p < PA ? a.ldx : a.ldw) + (DMA ? kc : 0)) * ES);
   }
   // the offset of K-tile s; behind the reduction's end out of range: zeros, by the same number of loads
   auto tile_off = [&](int s) { return s * KT + kc < a.K ? (uint32_t)(s * KT * ES) : OOB; };
@@ -294,11 +317,13 @@ __global__ void __launch_bounds__(WM * WN * 64) k_linear_tile(LinearArgs a) {
       const uint32_t kb = tile_off(s);
       static_for<0, PA + PB>([&](auto p) { fetch_piece(p, kb, buf * BUF); });
     } else {
+      auto row = [&](int p) { return reinterpret_cast<const T*>(reinterpret_cast<const char*>(p < PA ? xb : wb) + off[p]); };
+      if (k0 + KT <= a.K) {  // the same for the whole workgroup
 #pragma unroll
-      for (int p = 0; p < PA + PB; ++p) {
-        const int r = prow + (p < PA ? p : p - PA) * (NT / 8);
-        const bool ok = p < PA ? m0 + r < a.M : n0 + r < a.N;
-        reg[p] = ok ? piece(p < PA ? xb + r * a.ldx : wb + r * a.ldw, k0 + kc, a.K) : u32x4{0, 0, 0, 0};
+        for (int p = 0; p < PA + PB; ++p) reg[p] = full_piece(row(p), k0 + kc);
+      } else {
+#pragma unroll
+        for (int p = 0; p < PA + PB; ++p) reg[p] = piece(row(p), k0 + kc, a.K);
       }
     }
   };
@@ -463,7 +488,7 @@ __global__ void __launch_bounds__(WM * WN * 64) k_linear_tile(LinearArgs a) {
   // The finished tile through LDS, a block of 32 rows per wave row at a time, so that
   // whole rows are written.  Block (i, j): lane l holds row l % 32 and
   // features 8 g + 4 (l / 32) .. of g = 0 .. 3.  On the way out a thread keeps its 4
-  // features and walks the rows; the residuals of the rows to come are on their way.
+  // features and walks the rows, whose residuals are loaded before the block is put down.
   float* const out = reinterpret_cast<float*>(lds);
   constexpr int TR = NT / (BN / 4), PASSES = WM * 32 / TR;  // rows per pass
   const int n = n0 + tid % (BN / 4) * 4, r0 = tid / (BN / 4);
@@ -473,7 +498,9 @@ __global__ void __launch_bounds__(WM * WN * 64) k_linear_tile(LinearArgs a) {
       const int r = pass * TR + r0;
       return m0 + (r / 32 * FM + i) * 32 + r % 32;
     };
-    floatx4 res = residual4(a, row(0), n);
+    floatx4 res[PASSES];
+#pragma unroll
+    for (int pass = 0; pass < PASSES; ++pass) res[pass] = residual4(a, row(pass), n);
     __syncthreads();
 #pragma unroll
     for (int ii = 0; ii < FM; ++ii)
@@ -485,12 +512,9 @@ __global__ void __launch_bounds__(WM * WN * 64) k_linear_tile(LinearArgs a) {
             *reinterpret_cast<floatx4*>(out + (wm * 32 + fr) * PITCH + (wn * FN + j) * 32 + 8 * g + 4 * fq) =
                 floatx4{acc[ii][j][4 * g], acc[ii][j][4 * g + 1], acc[ii][j][4 * g + 2], acc[ii][j][4 * g + 3]};
     __syncthreads();
-#pragma unroll 2
-    for (int pass = 0; pass < PASSES; ++pass) {
-      const floatx4 now = res;
-      if (pass + 1 < PASSES) res = residual4(a, row(pass + 1), n);
-      finish4(a, row(pass), n, *reinterpret_cast<const floatx4*>(out + (pass * TR + r0) * PITCH + n - n0), bias, now);
-    }
+#pragma unroll
+    for (int pass = 0; pass < PASSES; ++pass)
+      finish4(a, row(pass), n, *reinterpret_cast<const floatx4*>(out + (pass * TR + r0) * PITCH + n - n0), bias, res[pass]);
   }
 }
 
@@ -509,13 +533,15 @@ void tile(const LinearArgs& a, hipStream_t s) {
 template <class T>
 void launch_t(const LinearArgs& a, hipStream_t s) {
   constexpr int VEC = LinT<T>::VEC;
-  // the loads that write LDS move 16 aligned bytes, at 31-bit offsets from a tile's first row
+  // the loads that write LDS move 16 aligned bytes
   const bool dma = a.K % VEC == 0 && a.ldx % VEC == 0 && a.ldw % VEC == 0 && reinterpret_cast<uintptr_t>(a.x) % 16 == 0 &&
-                   reinterpret_cast<uintptr_t>(a.w) % 16 == 0 && std::max(a.ldx, a.ldw) < (int64_t(1) << 31) / (256 * (int64_t)sizeof(T)) - a.K;
+                   reinterpret_cast<uintptr_t>(a.w) % 16 == 0;
+  // a tile of 256 rows is addressed by 31-bit offsets from its first one
+  const bool near = (255 * std::max(a.ldx, a.ldw) + a.K) * (int64_t)sizeof(T) < (int64_t(1) << 31);
   auto tiles = [&](int64_t bm, int64_t bn) { return (a.M + bm - 1) / bm * ((a.N + bn - 1) / bn); };
   if (a.M <= 16) return few<T, 1, 1, 8, 4>(a, s);
   if (a.M <= 32) return few<T, 2, 1, 8, 4>(a, s);
-  if (tiles(64, 64) < 128) return few<T, 2, 2, 8, 2>(a, s);
+  if (!near || tiles(64, 64) < 128) return few<T, 2, 2, 8, 2>(a, s);
   if (dma) {
     if (tiles(256, 256) >= 200) return tile<T, 256, 256, 2, 4, true, 2>(a, s);
     if (tiles(128, 128) >= 200) return tile<T, 128, 128, 2, 2, true, 2>(a, s);

@@ -1714,6 +1714,7 @@ void check_rows(const void* logits, int64_t ld, int32_t R, int32_t C) {
   if (R < 0 || C < 1) fail(FS_ERR_INVALID, "R must be >= 0 and C >= 1");
   if (R > 0 && !logits) fail(FS_ERR_INVALID, "logits are required");
   if (ld < C) fail(FS_ERR_INVALID, "ld must be >= C");
+  if (ld > int64_t(1) << 40) fail(FS_ERR_UNSUPPORTED, "row distances up to 2^40");
 }
 
 void check_teacher(const DistillArgs& a) {
@@ -1721,6 +1722,7 @@ void check_teacher(const DistillArgs& a) {
   if (a.R > 0 && (!a.ids || !a.u)) fail(FS_ERR_INVALID, "top_ids and top_logp are required");
   if (!(a.temperature >= 1e-6f && a.temperature <= 1e6f)) fail(FS_ERR_INVALID, "temperature must be in 1e-6..1e6");
   if (a.grad && a.ldg < a.C) fail(FS_ERR_INVALID, "ldg must be >= C");
+  if (a.grad && a.ldg > int64_t(1) << 40) fail(FS_ERR_UNSUPPORTED, "row distances up to 2^40");
   if (a.grad == a.z && a.grad && a.ldg != a.ld) fail(FS_ERR_INVALID, "a gradient over the logits needs ldg = ld");
 }
 
@@ -1740,6 +1742,7 @@ fs_status fs_linear_device(const void* d_x, int64_t ldx, const void* d_w, int64_
     if (activation < FS_ACT_NONE || activation > FS_ACT_SILU) fail(FS_ERR_INVALID, "unknown activation");
     if (M < 0 || N < 0 || K < 0) fail(FS_ERR_INVALID, "sizes must be >= 0");
     if (M > 1 << 26 || N > 1 << 26 || K > 1 << 30) fail(FS_ERR_UNSUPPORTED, "M and N up to 2^26, K up to 2^30");
+    if (std::max({ldx, ldw, ldres, ldy}) > int64_t(1) << 40) fail(FS_ERR_UNSUPPORTED, "row distances up to 2^40");
     if (ldx < K || ldw < K || ldy < N || (d_res && ldres != 0 && ldres < N))
       fail(FS_ERR_INVALID, "a row distance is shorter than its row");
     if (M == 0 || N == 0) return;
