@@ -530,26 +530,75 @@ void tile(const LinearArgs& a, hipStream_t s) {
   hipLaunchKernelGGL((k_linear_tile<T, BM, BN, WM, WN, DMA, NBUF>), dim3((unsigned)tiles), dim3(WM * WN * 64), 0, s, a);
 }
 
+// The kernels of more than 32 rows, and what a K-tile (128 bytes of a row) costs
+// one workgroup of each, in us: one / `fit` of them on a CU, measured at 128 to 4096
+// rows, 4096 features and K = 4096, and what a round of workgroups costs besides.
+// One row per kernel, by type and by how the loads go.
+enum Kernel { FEW_32x32, FEW_64x32, TILE_64x64, TILE_64x128, TILE_128x128, TILE_256x128, TILE_256x256, KERNELS };
+struct Cost {
+  int bm, bn, fit;
+  float alone, full, round;
+};
+// Where a kernel is not built, its cost is 0.
+constexpr Cost COSTS[2][2][KERNELS] = {
+    {   // bf16, loads through registers
+     {{32, 32, 2, .60f, 1.18f, 2.5f}, {64, 32, 2, .88f, 1.75f, 2.5f}, {64, 64, 4, 1.02f, 1.65f, 3.f}, {}, {128, 128, 2, 1.72f, 1.74f, 6.f}, {}, {256, 256, 1, 3.1f, 3.1f, 16.f}},
+        // bf16, loads into LDS
+     {{32, 32, 2, .245f, .456f, 2.5f}, {64, 32, 2, .345f, .67f, 2.5f}, {64, 64, 2, .33f, .50f, 3.f}, {64, 128, 2, .44f, .74f, 4.f}, {128, 128, 2, .62f, 1.03f, 7.f}, {256, 128, 1, .94f, .94f, 9.f}, {256, 256, 1, 1.48f, 1.48f, 16.f}}},
+    {   // fp32, loads through registers
+     {{32, 32, 2, .28f, .53f, 2.5f}, {64, 32, 2, .50f, .99f, 2.5f}, {64, 64, 2, 1.28f, 1.5f, 3.f}, {}, {128, 128, 2, 3.1f, 4.35f, 6.f}, {}, {256, 256, 1, 8.2f, 8.2f, 16.f}},
+        // fp32, loads into LDS: the matrix cores' rate, 7.4 us for 256 x 256 outputs
+     {{32, 32, 2, .277f, .53f, 2.5f}, {64, 32, 2, .50f, .97f, 2.5f}, {64, 64, 2, 1.15f, 1.22f, 3.f}, {64, 128, 2, 1.13f, 2.26f, 4.f}, {128, 128, 2, 2.06f, 3.95f, 6.f}, {256, 128, 1, 3.85f, 3.85f, 9.f}, {256, 256, 1, 7.45f, 7.45f, 16.f}}},
+};
+
+// The kernel with the least time by those costs: whole rounds of the chip and the
+// rest.  (bf16, K = 4096: 512 x 4096 outputs 64 x 128 32 us against 36 for 64 x 64 and
+// 44 for 128 x 128; 1024 x 4096 128 x 128 45 against 66 and, 256 x 256, 86; 2048 x 4096
+// 256 x 128 69 against 75 and 91; 4096 x 4096 256 x 256 114 against 134 for 256 x 128.)
+Kernel pick(const LinearArgs& a, bool f32, bool dma, bool near) {
+  const int64_t steps = ((int64_t)a.K * (f32 ? 4 : 2) + ROW - 1) / ROW;
+  Kernel best = FEW_32x32;
+  double least = 0;
+  for (int k = 0; k < (near ? KERNELS : TILE_64x64); ++k) {
+    const Cost& c = COSTS[f32][dma][k];
+    if (!c.bm) continue;
+    const int64_t n = ((a.M + c.bm - 1) / c.bm) * (int64_t)((a.N + c.bn - 1) / c.bn), round = 256 * c.fit;
+    const int64_t whole = n / round, rest = n % round;
+    // more than one on some CUs: the slowest CU's time, or, for the kernels bound by L2, a share of all
+    double last = rest <= 256 ? c.alone : c.full;
+    if (k < TILE_64x64 && rest > 256) last = c.alone + (c.full - c.alone) * (double)(rest - 256) / (double)(round - 256);
+    const double t = whole * (steps * (double)c.full + c.round) + (rest ? steps * last + c.round : 0);
+    if (k == 0 || t < least) {
+      least = t;
+      best = Kernel(k);
+    }
+  }
+  return best;
+}
+
 template <class T>
 void launch_t(const LinearArgs& a, hipStream_t s) {
   constexpr int VEC = LinT<T>::VEC;
+  constexpr bool F = sizeof(T) == 4;
   // the loads that write LDS move 16 aligned bytes
   const bool dma = a.K % VEC == 0 && a.ldx % VEC == 0 && a.ldw % VEC == 0 && reinterpret_cast<uintptr_t>(a.x) % 16 == 0 &&
                    reinterpret_cast<uintptr_t>(a.w) % 16 == 0;
   // a tile of 256 rows is addressed by 31-bit offsets from its first one
   const bool near = (255 * std::max(a.ldx, a.ldw) + a.K) * (int64_t)sizeof(T) < (int64_t(1) << 31);
-  auto tiles = [&](int64_t bm, int64_t bn) { return (a.M + bm - 1) / bm * ((a.N + bn - 1) / bn); };
-  if (a.M <= 16) return few<T, 1, 1, 8, 4>(a, s);
+  // up to 32 rows the weights are read once, 16 features a workgroup, and time is that of
+  // reading them (4096 features, K = 25088, bf16: 37 us for one row, 5.5 TB/s; 16
+  // waves against 8: 37 against 42 us) and, at 32 rows, of every workgroup reading x (70 us)
+  if (a.M <= 16) return few<T, 1, 1, 16, 2>(a, s);
   if (a.M <= 32) return few<T, 2, 1, 8, 4>(a, s);
-  if (!near || tiles(64, 64) < 128) return few<T, 2, 2, 8, 2>(a, s);
-  if (dma) {
-    if (tiles(256, 256) >= 200) return tile<T, 256, 256, 2, 4, true, 2>(a, s);
-    if (tiles(128, 128) >= 200) return tile<T, 128, 128, 2, 2, true, 2>(a, s);
-    return tile<T, 64, 64, 1, 2, true, 4>(a, s);
+  switch (pick(a, F, dma, near)) {
+    case FEW_32x32: return few<T, 2, 2, 8, 2>(a, s);
+    case FEW_64x32: return few<T, 4, 2, 8, 1>(a, s);
+    case TILE_64x64: return dma ? tile<T, 64, 64, 1, 2, true, 4>(a, s) : tile<T, 64, 64, 2, 2, false, 2>(a, s);
+    case TILE_64x128: return tile<T, 64, 128, 1, 4, true, 3>(a, s);
+    case TILE_128x128: return dma ? tile<T, 128, 128, 2, 2, true, 2>(a, s) : tile<T, 128, 128, 2, 2, false, 2>(a, s);
+    case TILE_256x128: return tile<T, 256, 128, 2, 4, true, 3>(a, s);
+    default: return dma ? tile<T, 256, 256, 2, 4, true, 2>(a, s) : tile<T, 256, 256, 2, 4, false, 2>(a, s);
   }
-  if (tiles(256, 256) >= 200) return tile<T, 256, 256, 2, 4, false, 2>(a, s);
-  if (tiles(128, 128) >= 200) return tile<T, 128, 128, 2, 2, false, 2>(a, s);
-  return tile<T, 64, 64, 2, 2, false, 2>(a, s);
 }
 
 }  // namespace
