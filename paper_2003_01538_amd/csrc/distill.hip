@@ -2,110 +2,451 @@
 // teacher entries and p that of its logits, both at a temperature,
 //   loss = sum_j q_j (ln q_j - ln p[id_j]),
 //   d loss / d logits_c = (p_c - sum of q_j with id_j = c) / temperature.
-// One workgroup per row.
+//
+// Memory bounds all of it, so the row is read once wherever it can be: a workgroup
+// holds its row in registers (k_distill_held: up to 256 KB of a CU's 512) between the
+// statistics and the gradient.  Longer rows are read twice (k_distill_long), the
+// second time mostly from the last-level cache.  Few long rows are cut into segments
+// for more workgroups: one launch for the statistics, through the scratch memory,
+// and one for loss and gradient.  The gradient alone, from given statistics, is one
+// pass in segments.
+//
+// The gradient is written as weight / temperature * p everywhere, then, after a
+// barrier of the workgroup that wrote them, again at the teacher's classes, where all
+// entries of a class write the same value.
 #include "rows.hpp"
 
+#include "flexserve.h"
+
+#include <algorithm>
 
 namespace fs {
 
 namespace {
 
-constexpr int ROW_T = 256;
+// Two maxima or sums over the workgroup at the price of one.
+template <int NT>
+__device__ __forceinline__ void block_max2(float& a, float& b, float (*sh)[2]) {
+  a = row_wave_max(a);
+  b = row_wave_max(b);
+  if constexpr (NT > 64) {
+    if ((threadIdx.x & 63) == 0) { sh[threadIdx.x >> 6][0] = a; sh[threadIdx.x >> 6][1] = b; }
+    __syncthreads();
+    a = sh[0][0]; b = sh[0][1];
+#pragma unroll
+    for (int w = 1; w < NT / 64; ++w) { a = fmaxf(a, sh[w][0]); b = fmaxf(b, sh[w][1]); }
+    __syncthreads();
+  }
+}
+template <int NT>
+__device__ __forceinline__ void block_sum2(float& a, float& b, float (*sh)[2]) {
+  a = row_wave_sum(a);
+  b = row_wave_sum(b);
+  if constexpr (NT > 64) {
+    if ((threadIdx.x & 63) == 0) { sh[threadIdx.x >> 6][0] = a; sh[threadIdx.x >> 6][1] = b; }
+    __syncthreads();
+    a = b = 0.f;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) { a += sh[w][0]; b += sh[w][1]; }
+    __syncthreads();
+  }
+}
+
+// The teacher's entries of a row, entry n NT + t with thread t, and what the
+// workgroup shares of them.
+template <int NT>
+struct Shared {
+  float red[NT / 64][2], q[MAX_TOP];
+  int id[MAX_TOP];
+};
+template <class T, int NT>
+struct Teacher {
+  static constexpr int E = (MAX_TOP + NT - 1) / NT;
+  int id[E];    // -1: none, or left out
+  float u[E];   // then e^((u - max) c), then q
+  float z[E];   // the student's logit of the class
+
+  __device__ __forceinline__ void load(const DistillArgs& a, int64_t row, const T* zr) {
+#pragma unroll
+    for (int n = 0; n < E; ++n) {
+      const int j = n * NT + threadIdx.x;
+      id[n] = j < a.K ? a.ids[row * a.K + j] : -1;
+      u[n] = j < a.K ? a.u[row * a.K + j] : -INFINITY;
+      if (id[n] < 0 || id[n] >= a.C) { id[n] = -1; u[n] = -INFINITY; }
+    }
+#pragma unroll
+    for (int n = 0; n < E; ++n) z[n] = id[n] >= 0 && zr ? RowT<T>::one(zr + id[n]) : -INFINITY;
+  }
+  __device__ __forceinline__ float max() const {
+    float m = -FLT_MAX;
+#pragma unroll
+    for (int n = 0; n < E; ++n) m = fmaxf(m, u[n]);
+    return m;
+  }
+  __device__ __forceinline__ float exps(float m, float k2) {
+    float s = 0.f;
+#pragma unroll
+    for (int n = 0; n < E; ++n) {
+      u[n] = __builtin_amdgcn_exp2f((u[n] - m) * k2);
+      s += u[n];
+    }
+    return s;
+  }
+  // q, given the sum of exps(); visible to the workgroup after its next barrier
+  __device__ __forceinline__ void share(float s, Shared<NT>& S) {
+    const float inv = s == 0.f ? 0.f : 1.f / s;
+#pragma unroll
+    for (int n = 0; n < E; ++n) {
+      const int j = n * NT + threadIdx.x;
+      u[n] = id[n] < 0 ? 0.f : u[n] * inv;
+      if (j < MAX_TOP) { S.q[j] = u[n]; S.id[j] = id[n]; }
+    }
+  }
+};
+
+// (m, l): the row's statistics, l = ln s; m is -inf in a row without classes
+struct Stats {
+  float m, l;
+};
+__device__ __forceinline__ Stats stats_of(float m, float s) { return s == 0.f ? Stats{-INFINITY, 0.f} : Stats{m, logf(s)}; }
+__device__ __forceinline__ float ln_p(const Stats& st, float z, float c) { return z == -INFINITY ? -INFINITY : (z - st.m) * c - st.l; }
+
+// This thread's part of the loss.
+template <class T, int NT>
+__device__ __forceinline__ float loss_part(const Teacher<T, NT>& t, const Stats& st, float c) {
+  float part = 0.f;
+#pragma unroll
+  for (int n = 0; n < Teacher<T, NT>::E; ++n)
+    if (t.id[n] >= 0 && t.u[n] != 0.f) part += t.u[n] * (logf(t.u[n]) - ln_p(st, t.z[n], c));
+  return part;
+}
+
+// The gradient without the teacher: scale * e^((z - m) c - l).  Rows whose
+// teacher has no mass are 0, as are classes at -inf whatever the row holds.
+struct Grad {
+  float m, k2, l2, scale;
+  bool zero, care;  // all 0; classes at -inf need a look
+  __device__ __forceinline__ Grad(const Stats& st, float c, float weight, bool mass)
+      : m(st.m), k2(LOG2E * c), l2(LOG2E * st.l), scale(weight * c), zero(!mass || st.m == -INFINITY),
+        care(!(fabsf(st.l) < INFINITY) || !(fabsf(scale) < INFINITY)) {}
+  __device__ __forceinline__ float at(float z) const {
+    const float p = __builtin_amdgcn_exp2f(fmaf(z - m, k2, -l2)) * scale;
+    return zero || (care && z == -INFINITY) ? 0.f : p;
+  }
+  template <class T>
+  __device__ __forceinline__ u32x4 vec(u32x4 v) const {
+    constexpr int VEC = RowT<T>::VEC;
+    float f[VEC];
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) f[e] = __builtin_amdgcn_exp2f(fmaf(RowT<T>::get(v, e) - m, k2, -l2)) * scale;
+    if (zero || care) {  // the same for the whole workgroup
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) f[e] = at(RowT<T>::get(v, e));
+    }
+    return RowT<T>::pack(f);
+  }
+};
 
 template <class T>
-__device__ void row_stats(const T* z, int C, float c, float* sh, float& m, float& s, float& t) {
-  float best = -FLT_MAX;
-  for (int i = threadIdx.x; i < C; i += ROW_T) best = fmaxf(best, RowT<T>::one(z + i));
-  m = block_max<ROW_T>(best, sh);
-  s = t = 0.f;
-  for (int i = threadIdx.x; i < C; i += ROW_T) s += expf((RowT<T>::one(z + i) - m) * c);
-  s = block_sum<ROW_T>(s, sh);
-}
-
-// The row's teacher in LDS: q[j] (0 for an entry that is left out) and id[j]
-// (-1 for one).  Returns whether the teacher has any mass.
-__device__ bool teacher(const DistillArgs& a, int64_t row, float c, float* q, int* id, float* sh) {
-  const int j = threadIdx.x;
-  float u = -INFINITY;
-  int k = -1;
-  if (j < a.K) {
-    k = a.ids[row * a.K + j];
-    if (k < 0 || k >= a.C) k = -1;
-    else u = a.u[row * a.K + j];
+__device__ __forceinline__ void put_vec(T* g, int64_t i, int64_t end, u32x4 v) {
+  constexpr int VEC = RowT<T>::VEC;
+  if (i + VEC <= end) {
+    RowT<T>::store(g + i, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e)
+      if (i + e < end) RowT<T>::put(g + i + e, RowT<T>::get(v, e));
   }
-  const bool mass = __syncthreads_or(!(u == -INFINITY));
-  const float m = block_max<ROW_T>(fmaxf(u, -FLT_MAX), sh);
-  const float e = k < 0 ? 0.f : expf((u - m) * c);
-  const float s = block_sum<ROW_T>(e, sh);
-  if (j < a.K) { q[j] = mass ? e / s : 0.f; id[j] = k; }
-  __syncthreads();
-  return mass;
 }
 
-template <class T, bool STATS>
-__global__ void __launch_bounds__(ROW_T) k_distill(DistillArgs a) {
-  __shared__ float sh[ROW_T / 64], q[MAX_TOP];
-  __shared__ int id[MAX_TOP];
-  const float c = 1.f / a.temperature;
+// The vectors that row_chunk loads, as gradients.
+template <class T, int NT, int NV>
+__device__ __forceinline__ void put_chunk(T* g, int64_t from, int64_t end, const u32x4 (&v)[NV], const Grad& gr) {
+  constexpr int VEC = RowT<T>::VEC;
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    const int64_t i = from + (int64_t)(j * NT + (int)threadIdx.x) * VEC;
+    const u32x4 q = gr.template vec<T>(v[j]);
+    if (from + (int64_t)(j + 1) * NT * VEC <= end) RowT<T>::store(g + i, q);  // the same for the whole workgroup
+    else put_vec(g, i, end, q);
+  }
+}
+
+// The gradient at the teacher's classes in first .. end - 1, after the barrier that follows
+// the others'.
+template <class T, int NT>
+__device__ __forceinline__ void put_teacher(const DistillArgs& a, T* g, const Teacher<T, NT>& t, const Shared<NT>& S, const Stats& st,
+                                            const Grad& gr, float c, int64_t first, int64_t end) {
+#pragma unroll
+  for (int n = 0; n < Teacher<T, NT>::E; ++n) {
+    const int k = t.id[n];
+    if (k < first || k >= end) continue;
+    float sum = 0.f;
+    for (int j = 0; j < a.K; ++j) sum += S.id[j] == k ? S.q[j] : 0.f;
+    const float p = st.m == -INFINITY || t.z[n] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(fmaf(t.z[n] - gr.m, gr.k2, -gr.l2));
+    RowT<T>::put(g + k, (p - sum) * gr.scale);
+  }
+}
+
+__device__ __forceinline__ float weight_of(const DistillArgs& a, int64_t row) { return a.weight ? a.weight[row] : 1.f; }
+
+// Rows of at most NT * NV vectors.
+template <class T, int NT, int NV>
+__global__ void __launch_bounds__(NT) k_distill_held(DistillArgs a) {
+  using RT = RowT<T>;
+  constexpr int VEC = RT::VEC;
+  __shared__ Shared<NT> S;
+  const float c = 1.f / a.temperature, k2 = LOG2E * c;
   for (int64_t row = blockIdx.x; row < a.R; row += gridDim.x) {
     const T* z = static_cast<const T*>(a.z) + row * a.ld;
-    const bool mass = teacher(a, row, c, q, id, sh);
-    float m, l;
-    if constexpr (STATS) {
-      float s, t;
-      row_stats(z, a.C, c, sh, m, s, t);
-      l = s == 0.f ? 0.f : logf(s);
-      if (s == 0.f) m = -INFINITY;
-      if (a.stats && threadIdx.x == 0) { a.stats[row * 2] = m; a.stats[row * 2 + 1] = l; }
-    } else {
-      m = a.stats[row * 2];
-      l = a.stats[row * 2 + 1];
-    }
-    // this thread's teacher entry: the student's logit and log probability there, read before any gradient is written
-    const int j = threadIdx.x;
-    const int cj = j < a.K ? id[j] : -1;
-    float lp = 0.f;
-    if (cj >= 0) {
-      const float x = RowT<T>::one(z + cj);
-      lp = x == -INFINITY ? -INFINITY : (x - m) * c - l;
-    }
-    if (STATS && a.loss) {
-      float part = 0.f;
-      if (cj >= 0 && q[j] != 0.f) part = q[j] * (logf(q[j]) - lp);
-      const float loss = block_sum<ROW_T>(part, sh);
-      if (threadIdx.x == 0) a.loss[row] = mass ? loss : 0.f;
+    u32x4 v[NV];
+    row_chunk<T, NT, NV>(z, 0, a.C, v);
+    Teacher<T, NT> t;
+    t.load(a, row, z);
+    float m = -FLT_MAX, um = t.max();
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) m = fmaxf(m, RT::get(v[j], e));
+    forget(v);
+    block_max2<NT>(m, um, S.red);
+    float s = 0.f, us = t.exps(um, k2);
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) s += __builtin_amdgcn_exp2f((RT::get(v[j], e) - m) * k2);
+    forget(v);
+    block_sum2<NT>(s, us, S.red);
+    t.share(us, S);
+    const Stats st = stats_of(m, s);
+    if (a.stats && threadIdx.x == 0) { a.stats[row * 2] = st.m; a.stats[row * 2 + 1] = st.l; }
+    if (a.loss) {
+      const float loss = block_sum<NT>(loss_part(t, st, c), &S.red[0][0]);
+      if (threadIdx.x == 0) a.loss[row] = loss;  // 0 without mass: every q is
     }
     if (a.grad) {
       T* g = static_cast<T*>(a.grad) + row * a.ldg;
-      const float wt = (a.weight ? a.weight[row] : 1.f) * c;
+      const Grad gr(st, c, weight_of(a, row), us != 0.f);
+      __syncthreads();  // the row and its teacher's classes have been read (the gradient may lie over them)
+      put_chunk<T, NT, NV>(g, 0, a.C, v, gr);
       __syncthreads();
-      for (int i = threadIdx.x; i < a.C; i += ROW_T) {
-        const float x = RowT<T>::one(z + i);
-        RowT<T>::put(g + i, !mass ? 0.f : x == -INFINITY ? 0.f : expf((x - m) * c - l) * wt);
-      }
-      __syncthreads();
-      if (mass && cj >= 0) {
-        float sum = 0.f;  // entries of one class write the same value
-        for (int i = 0; i < a.K; ++i) sum += id[i] == cj ? q[i] : 0.f;
-        RowT<T>::put(g + cj, (expf(lp) - sum) * wt);
-      }
+      if (us != 0.f) put_teacher<T, NT>(a, g, t, S, st, gr, c, 0, a.C);
     }
     __syncthreads();
   }
 }
 
+// Statistics of z[first .. end - 1] over the workgroup: m and s.
+template <class T, int NT, int NV>
+__device__ __forceinline__ RowStats<false> walk_stats(const T* z, int64_t first, int64_t end, float k2, float* sh) {
+  using RT = RowT<T>;
+  constexpr int VEC = RT::VEC, CHUNK = NT * NV * VEC;
+  RowStats<false> st;
+  u32x4 v[NV], next[NV];
+  row_chunk<T, NT, NV>(z, first, end, v);
+  for (int64_t from = first; from < end; from += CHUNK) {
+    const bool more = from + CHUNK < end;
+    if (more) row_chunk<T, NT, NV>(z, from + CHUNK, end, next);
+    float best = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) best = fmaxf(best, RT::get(v[j], e));
+    if (best > st.m) st.lift(best, k2);
+#pragma unroll
+    for (int j = 0; j < NV; ++j)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) st.add(RT::get(v[j], e), k2);
+    if (more)
+#pragma unroll
+      for (int j = 0; j < NV; ++j) v[j] = next[j];
+  }
+  st.over_block<NT>(k2, sh);
+  return st;
+}
+
+// The gradient without the teacher, of z[first .. end - 1].
+template <class T, int NT, int NV>
+__device__ __forceinline__ void walk_grad(const T* z, T* g, int64_t first, int64_t end, const Grad& gr) {
+  constexpr int CHUNK = NT * NV * RowT<T>::VEC;
+  u32x4 v[NV], next[NV];
+  row_chunk<T, NT, NV>(z, first, end, v);
+  for (int64_t from = first; from < end; from += CHUNK) {
+    const bool more = from + CHUNK < end;
+    if (more) row_chunk<T, NT, NV>(z, from + CHUNK, end, next);
+    put_chunk<T, NT, NV>(g, from, end, v, gr);
+    if (more)
+#pragma unroll
+      for (int j = 0; j < NV; ++j) v[j] = next[j];
+  }
+}
+
+// Rows of any length, read once for the statistics and once for the gradient.
+template <class T, int NT, int NV>
+__global__ void __launch_bounds__(NT) k_distill_long(DistillArgs a) {
+  __shared__ Shared<NT> S;
+  const float c = 1.f / a.temperature, k2 = LOG2E * c;
+  for (int64_t row = blockIdx.x; row < a.R; row += gridDim.x) {
+    const T* z = static_cast<const T*>(a.z) + row * a.ld;
+    Teacher<T, NT> t;
+    t.load(a, row, z);
+    const RowStats<false> rs = walk_stats<T, NT, NV>(z, 0, a.C, k2, &S.red[0][0]);
+    const Stats st = stats_of(rs.m, rs.s);
+    const float us = block_sum<NT>(t.exps(block_max<NT>(t.max(), &S.red[0][0]), k2), &S.red[0][0]);
+    t.share(us, S);
+    if (a.stats && threadIdx.x == 0) { a.stats[row * 2] = st.m; a.stats[row * 2 + 1] = st.l; }
+    if (a.loss) {
+      const float loss = block_sum<NT>(loss_part(t, st, c), &S.red[0][0]);
+      if (threadIdx.x == 0) a.loss[row] = loss;
+    }
+    if (a.grad) {
+      T* g = static_cast<T*>(a.grad) + row * a.ldg;
+      const Grad gr(st, c, weight_of(a, row), us != 0.f);
+      __syncthreads();
+      walk_grad<T, NT, NV>(z, g, 0, a.C, gr);
+      __syncthreads();
+      if (us != 0.f) put_teacher<T, NT>(a, g, t, S, st, gr, c, 0, a.C);
+    }
+    __syncthreads();
+  }
+}
+
+// The scratch memory of rows in segments: the segments' statistics, then the
+// students' logits at the teachers' classes, since the gradient may be written over
+// them before the loss is formed.
+struct Part {
+  float m, s;
+};
+__device__ __forceinline__ float* scratch_z(const DistillArgs& a, int segs) {
+  return reinterpret_cast<float*>(static_cast<Part*>(a.scratch) + (int64_t)a.R * segs);
+}
+
+template <class T, int NT, int NV>
+__global__ void __launch_bounds__(NT) k_distill_stats(DistillArgs a, int segs, int seg) {
+  __shared__ float sh[NT / 64];
+  const int row = blockIdx.x / segs, first = (blockIdx.x - row * segs) * seg;
+  const T* z = static_cast<const T*>(a.z) + (int64_t)row * a.ld;
+  if (first == 0)
+    for (int j = threadIdx.x; j < a.K; j += NT) {
+      const int k = a.ids[(int64_t)row * a.K + j];
+      scratch_z(a, segs)[(int64_t)row * a.K + j] = k >= 0 && k < a.C ? RowT<T>::one(z + k) : -INFINITY;
+    }
+  const RowStats<false> st = walk_stats<T, NT, NV>(z, first, min((int64_t)a.C, (int64_t)first + seg), LOG2E / a.temperature, sh);
+  if (threadIdx.x == 0) static_cast<Part*>(a.scratch)[blockIdx.x] = Part{st.m, st.s};
+}
+
+// Loss (the first segment's workgroup) and gradient of a segment.  PARTS: the
+// statistics are `parts` parts in the scratch memory; otherwise a.stats holds them.
+template <class T, int NT, int NV, bool PARTS>
+__global__ void __launch_bounds__(NT) k_distill_segment(DistillArgs a, int segs, int seg, int parts) {
+  __shared__ Shared<NT> S;
+  const float c = 1.f / a.temperature, k2 = LOG2E * c;
+  const int64_t items = (int64_t)a.R * segs;
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const int64_t row = item / segs, first = (item - row * segs) * seg, end = min((int64_t)a.C, first + seg);
+    const T* z = static_cast<const T*>(a.z) + row * a.ld;
+    Teacher<T, NT> t;
+    t.load(a, row, PARTS ? nullptr : z);
+    float us = block_sum<NT>(t.exps(block_max<NT>(t.max(), &S.red[0][0]), k2), &S.red[0][0]);
+    t.share(us, S);
+    Stats st;
+    if constexpr (PARTS) {
+      RowStats<false> rs;
+      for (int i = threadIdx.x; i < parts; i += NT) {
+        const Part p = static_cast<const Part*>(a.scratch)[row * parts + i];
+        RowStats<false> q;
+        q.m = p.m; q.s = p.s;
+        const float m = fmaxf(rs.m, q.m);
+        rs.lift(m, k2);
+        q.lift(m, k2);
+        rs.s += q.s;
+      }
+#pragma unroll
+      for (int n = 0; n < Teacher<T, NT>::E; ++n)
+        if (t.id[n] >= 0) t.z[n] = scratch_z(a, parts)[row * a.K + n * NT + threadIdx.x];
+      rs.over_block<NT>(k2, &S.red[0][0]);
+      st = stats_of(rs.m, rs.s);
+      if (first == 0) {
+        if (a.stats && threadIdx.x == 0) { a.stats[row * 2] = st.m; a.stats[row * 2 + 1] = st.l; }
+        if (a.loss) {
+          const float loss = block_sum<NT>(loss_part(t, st, c), &S.red[0][0]);
+          if (threadIdx.x == 0) a.loss[row] = loss;
+        }
+      }
+    } else {
+      st = Stats{a.stats[row * 2], a.stats[row * 2 + 1]};
+    }
+    if (a.grad) {
+      T* g = static_cast<T*>(a.grad) + row * a.ldg;
+      const Grad gr(st, c, weight_of(a, row), us != 0.f);
+      __syncthreads();  // this segment's classes of the teacher have been read
+      walk_grad<T, NT, NV>(z, g, first, end, gr);
+      __syncthreads();
+      if (us != 0.f) put_teacher<T, NT>(a, g, t, S, st, gr, c, first, end);
+    }
+    __syncthreads();
+  }
+}
+
+constexpr int64_t GRID = 1 << 20;  // workgroups walk the rows beyond
+constexpr int SEGS = 512;          // segments of all rows whose statistics are split
+static_assert(SEGS * (sizeof(Part) + MAX_TOP * sizeof(float)) <= FS_ROW_SCRATCH_BYTES, "scratch");
+
+// A row's segments: `want` of them, whole chunks each.
+struct Cut {
+  int segs, seg;
+};
+Cut cut_row(int C, int chunk, int64_t want) {
+  const int chunks = (int)(((int64_t)C + chunk - 1) / chunk);
+  const int n = (int)std::max<int64_t>(1, std::min<int64_t>(chunks, want));
+  const int per = (chunks + n - 1) / n;
+  return {(chunks + per - 1) / per, per * chunk};
+}
+
+template <class T, bool PARTS>
+void segments(const DistillArgs& a, Cut cut, int parts, hipStream_t s) {
+  const int64_t items = (int64_t)a.R * cut.segs;
+  hipLaunchKernelGGL((k_distill_segment<T, 256, 4, PARTS>), dim3((unsigned)std::min(items, GRID)), dim3(256), 0, s, a, cut.segs, cut.seg, parts);
+}
+
+template <class T, int NT, int NV>
+void held(const DistillArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((k_distill_held<T, NT, NV>), dim3((unsigned)std::min<int64_t>(a.R, GRID)), dim3(NT), 0, s, a);
+}
+
+template <class T>
+void launch_t(const DistillArgs& a, hipStream_t s) {
+  constexpr int VEC = RowT<T>::VEC, CHUNK = 256 * 4 * VEC;
+  if (a.C <= 64 * 4 * VEC) return held<T, 64, 4>(a, s);
+  if (a.C <= 256 * 4 * VEC) return held<T, 256, 4>(a, s);
+  if (a.scratch && a.R <= 64) {
+    const Cut cut = cut_row(a.C, CHUNK, SEGS / a.R);
+    if (cut.segs > 1) {
+      hipLaunchKernelGGL((k_distill_stats<T, 256, 4>), dim3((unsigned)(a.R * cut.segs)), dim3(256), 0, s, a, cut.segs, cut.seg);
+      return segments<T, true>(a, a.grad ? cut : Cut{1, a.C}, cut.segs, s);
+    }
+  }
+  if (a.C <= 256 * 16 * VEC) return held<T, 256, 16>(a, s);
+  if (a.C <= 1024 * 16 * VEC) return held<T, 1024, 16>(a, s);
+  hipLaunchKernelGGL((k_distill_long<T, 1024, 4>), dim3((unsigned)std::min<int64_t>(a.R, GRID)), dim3(1024), 0, s, a);
+}
+
+template <class T>
+void launch_grad_t(const DistillArgs& a, hipStream_t s) {
+  constexpr int CHUNK = 256 * 4 * RowT<T>::VEC;
+  segments<T, false>(a, cut_row(a.C, CHUNK, std::max<int64_t>(1, 4096 / a.R)), 0, s);
+}
+
 }  // namespace
 
 void launch_distill(const DistillArgs& a, Prec p, hipStream_t s) {
-  const dim3 grid(a.R < (1 << 20) ? a.R : 1 << 20);
-  if (p == BF16) hipLaunchKernelGGL((k_distill<uint16_t, true>), grid, dim3(ROW_T), 0, s, a);
-  else hipLaunchKernelGGL((k_distill<float, true>), grid, dim3(ROW_T), 0, s, a);
+  if (p == BF16) launch_t<uint16_t>(a, s);
+  else launch_t<float>(a, s);
 }
 
 void launch_distill_grad(const DistillArgs& a, Prec p, hipStream_t s) {
-  const dim3 grid(a.R < (1 << 20) ? a.R : 1 << 20);
-  if (p == BF16) hipLaunchKernelGGL((k_distill<uint16_t, false>), grid, dim3(ROW_T), 0, s, a);
-  else hipLaunchKernelGGL((k_distill<float, false>), grid, dim3(ROW_T), 0, s, a);
+  if (p == BF16) launch_grad_t<uint16_t>(a, s);
+  else launch_grad_t<float>(a, s);
 }
 
 }  // namespace fs

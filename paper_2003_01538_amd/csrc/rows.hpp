@@ -68,13 +68,20 @@ __device__ __forceinline__ u32x4 row_vec(const T* z, int64_t i, int64_t end) {
 template <class T, int NT, int NV>
 __device__ __forceinline__ void row_chunk(const T* z, int64_t from, int64_t end, u32x4 (&v)[NV]) {
   constexpr int VEC = RowT<T>::VEC;
-  if (from + NT * NV * VEC <= end) {  // the same for the whole workgroup
 #pragma unroll
-    for (int j = 0; j < NV; ++j) v[j] = RowT<T>::load(z + from + (j * NT + (int)threadIdx.x) * VEC);
-  } else {
-#pragma unroll
-    for (int j = 0; j < NV; ++j) v[j] = row_vec(z, from + (j * NT + (int)threadIdx.x) * VEC, end);
+  for (int j = 0; j < NV; ++j) {
+    const int64_t i = from + (int64_t)(j * NT + (int)threadIdx.x) * VEC;
+    if (from + (int64_t)(j + 1) * NT * VEC <= end) v[j] = RowT<T>::load(z + i);  // the same for the whole workgroup
+    else v[j] = row_vec(z, i, end);
   }
+}
+
+// What a phase made of the vectors (fp32 logits, masks) is formed again in the next
+// instead of being kept in registers.
+template <int NV>
+__device__ __forceinline__ void forget(u32x4 (&v)[NV]) {
+#pragma unroll
+  for (int j = 0; j < NV; ++j) __asm__ volatile("" : "+v"(v[j]));
 }
 
 // Wavefront reductions in registers: within rows of 16 lanes, then a row's last

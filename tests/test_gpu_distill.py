@@ -79,7 +79,9 @@ class Call:
         scale = np.abs(1.0 if self.weight is None else self.weight.cpu().numpy()) / self.tau
         # values in [1, 2) lie 2^-7 (bf16) or 2^-23 (fp32) apart: half a step is at most 2^-8 or 2^-24 of the value
         half = 2.0 ** -8 if self.prec == BF else U
-        tol = off * np.reshape(scale, (-1, 1) if np.ndim(scale) else (1, 1)) + (half + 3 * U) * np.abs(np.nan_to_num(w["grad"])) + 1e-37
+        # an exponential below 2^-126, the least normal fp32 number, may be 0: times scale in the gradient
+        least = 2.0 ** -126 * np.reshape(scale, (-1, 1) if np.ndim(scale) else (1, 1))
+        tol = off * np.reshape(scale, (-1, 1) if np.ndim(scale) else (1, 1)) + (half + 3 * U) * np.abs(np.nan_to_num(w["grad"])) + least + 1e-37
         near(self.grad.numpy(), w["grad"], tol)
         assert self.grad.untouched()
         return self
