@@ -147,18 +147,6 @@ struct Grad {
   }
 };
 
-template <class T>
-__device__ __forceinline__ void put_vec(T* g, int64_t i, int64_t end, u32x4 v) {
-  constexpr int VEC = RowT<T>::VEC;
-  if (i + VEC <= end) {
-    RowT<T>::store(g + i, v);
-  } else {
-#pragma unroll
-    for (int e = 0; e < VEC; ++e)
-      if (i + e < end) RowT<T>::put(g + i + e, RowT<T>::get(v, e));
-  }
-}
-
 // The vectors that row_chunk loads, as gradients.
 template <class T, int NT, int NV>
 __device__ __forceinline__ void put_chunk(T* g, int64_t from, int64_t end, const u32x4 (&v)[NV], const Grad& gr) {
@@ -199,8 +187,9 @@ __global__ void __launch_bounds__(NT) k_distill_held(DistillArgs a) {
   const float c = 1.f / a.temperature, k2 = LOG2E * c;
   for (int64_t row = blockIdx.x; row < a.R; row += gridDim.x) {
     const T* z = static_cast<const T*>(a.z) + row * a.ld;
+    const int C = row_end(a.C);
     u32x4 v[NV];
-    row_chunk<T, NT, NV>(z, 0, a.C, v);
+    row_chunk<T, NT, NV>(z, 0, C, v);
     Teacher<T, NT> t;
     t.load(a, row, z);
     float m = -FLT_MAX, um = t.max();
@@ -228,7 +217,7 @@ __global__ void __launch_bounds__(NT) k_distill_held(DistillArgs a) {
       T* g = static_cast<T*>(a.grad) + row * a.ldg;
       const Grad gr(st, c, weight_of(a, row), us != 0.f);
       __syncthreads();  // the row and its teacher's classes have been read (the gradient may lie over them)
-      put_chunk<T, NT, NV>(g, 0, a.C, v, gr);
+      put_chunk<T, NT, NV>(g, 0, row_end(C), v, gr);
       __syncthreads();
       if (us != 0.f) put_teacher<T, NT>(a, g, t, S, st, gr, c, 0, a.C);
     }
@@ -290,7 +279,7 @@ __global__ void __launch_bounds__(NT) k_distill_long(DistillArgs a) {
     const T* z = static_cast<const T*>(a.z) + row * a.ld;
     Teacher<T, NT> t;
     t.load(a, row, z);
-    const RowStats<false> rs = walk_stats<T, NT, NV>(z, 0, a.C, k2, &S.red[0][0]);
+    const RowStats<false> rs = walk_stats<T, NT, NV>(z, 0, row_end(a.C), k2, &S.red[0][0]);
     const Stats st = stats_of(rs.m, rs.s);
     const float us = block_sum<NT>(t.exps(block_max<NT>(t.max(), &S.red[0][0]), k2), &S.red[0][0]);
     t.share(us, S);
@@ -303,7 +292,7 @@ __global__ void __launch_bounds__(NT) k_distill_long(DistillArgs a) {
       T* g = static_cast<T*>(a.grad) + row * a.ldg;
       const Grad gr(st, c, weight_of(a, row), us != 0.f);
       __syncthreads();
-      walk_grad<T, NT, NV>(z, g, 0, a.C, gr);
+      walk_grad<T, NT, NV>(z, g, 0, row_end(a.C), gr);
       __syncthreads();
       if (us != 0.f) put_teacher<T, NT>(a, g, t, S, st, gr, c, 0, a.C);
     }

@@ -267,7 +267,7 @@ __global__ void __launch_bounds__(NT) k_logprob(LogprobArgs a, int segs, int seg
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
     const int64_t row = SPLIT ? item / segs : item;
     const int64_t first = SPLIT ? (item - row * segs) * seg : 0;
-    const int64_t end = SPLIT ? min((int64_t)a.C, first + seg) : a.C;
+    const int64_t end = SPLIT ? min((int64_t)a.C, first + seg) : row_end(a.C);
     const T* z = static_cast<const T*>(a.z) + row * a.ld;
     select_begin(S);
     RowStats<true> st;

@@ -24,6 +24,10 @@ constexpr float FAR = -200.f;  // e^FAR is 0 in fp32: a bound for z - m where it
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef u32x4 u32x4_at2 __attribute__((aligned(2)));
 typedef u32x4 u32x4_at4 __attribute__((aligned(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef u32x2 u32x2_at2 __attribute__((aligned(2)));
+typedef u32x2 u32x2_at4 __attribute__((aligned(4)));
+typedef uint32_t u32_at2 __attribute__((aligned(2)));
 
 template <class T> struct RowT;
 template <> struct RowT<float> {
@@ -52,15 +56,61 @@ template <> struct RowT<uint16_t> {  // bf16
   }
 };
 
-// Elements i .. i + VEC - 1 of a row that ends at `end`; -inf behind the end.
+// Elements i .. i + VEC - 1 of a row that ends at `end`; -inf behind the end.  A
+// row's last vector is put together from pieces of 4, 2 and 1 elements, the last first.
 template <class T>
 __device__ __forceinline__ u32x4 row_vec(const T* z, int64_t i, int64_t end) {
   constexpr int VEC = RowT<T>::VEC;
   if (i + VEC <= end) return RowT<T>::load(z + i);
-  float f[VEC];
-#pragma unroll
-  for (int e = 0; e < VEC; ++e) f[e] = i + e < end ? RowT<T>::one(z + i + e) : -INFINITY;
-  return RowT<T>::pack(f);
+  const int r = (int)(end > i ? end - i : 0);
+  const T* p = z + i;
+  if constexpr (VEC == 8) {
+    uint64_t lo = 0xff80ff80ff80ff80ull, hi = lo;  // -inf
+    if (r & 1) {
+      hi = hi << 16 | lo >> 48;
+      lo = lo << 16 | p[r & 6];
+    }
+    if (r & 2) {
+      const uint32_t w = *reinterpret_cast<const u32_at2*>(p + (r & 4));
+      hi = hi << 32 | lo >> 32;
+      lo = lo << 32 | w;
+    }
+    if (r & 4) {
+      const u32x2 w = *reinterpret_cast<const u32x2_at2*>(p);
+      hi = lo;
+      lo = w[0] | uint64_t(w[1]) << 32;
+    }
+    return u32x4{uint32_t(lo), uint32_t(lo >> 32), uint32_t(hi), uint32_t(hi >> 32)};
+  } else {
+    constexpr uint32_t NEG = 0xff800000u;  // -inf
+    u32x4 v = {NEG, NEG, NEG, NEG};
+    if (r & 1) v[0] = __float_as_uint(p[r & 2]);
+    if (r & 2) {
+      const u32x2 w = *reinterpret_cast<const u32x2_at4*>(p);
+      v = u32x4{w[0], w[1], v[0], NEG};
+    }
+    return v;
+  }
+}
+
+// ... and those of the vector's elements that lie before the end, written.
+template <class T>
+__device__ __forceinline__ void put_vec(T* g, int64_t i, int64_t end, u32x4 v) {
+  constexpr int VEC = RowT<T>::VEC;
+  if (i + VEC <= end) {
+    RowT<T>::store(g + i, v);
+    return;
+  }
+  const int r = (int)(end > i ? end - i : 0);
+  T* p = g + i;
+  if constexpr (VEC == 8) {
+    if (r & 4) *reinterpret_cast<u32x2_at2*>(p) = u32x2{v[0], v[1]};
+    if (r & 2) *reinterpret_cast<u32_at2*>(p + (r & 4)) = r & 4 ? v[2] : v[0];
+    if (r & 1) p[r & 6] = (uint16_t)(r & 4 ? (r & 2 ? v[3] : v[2]) : (r & 2 ? v[1] : v[0]));
+  } else {
+    if (r & 2) *reinterpret_cast<u32x2_at4*>(p) = u32x2{v[0], v[1]};
+    if (r & 1) p[r & 2] = __uint_as_float(r & 2 ? v[2] : v[0]);
+  }
 }
 
 // NV vectors of a workgroup's chunk of NT * NV vectors that begins at `from`:
@@ -74,6 +124,13 @@ __device__ __forceinline__ void row_chunk(const T* z, int64_t from, int64_t end,
     if (from + (int64_t)(j + 1) * NT * VEC <= end) v[j] = RowT<T>::load(z + i);  // the same for the whole workgroup
     else v[j] = row_vec(z, i, end);
   }
+}
+
+// A row's length, formed again for every row, so that nothing that follows from it
+// for a thread's vectors is kept in registers from row to row.
+__device__ __forceinline__ int row_end(int C) {
+  __asm__ volatile("" : "+s"(C));
+  return C;
 }
 
 // What a phase made of the vectors (fp32 logits, masks) is formed again in the next
