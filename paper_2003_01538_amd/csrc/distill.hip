@@ -178,9 +178,10 @@ __device__ __forceinline__ void put_teacher(const DistillArgs& a, T* g, const Te
 
 __device__ __forceinline__ float weight_of(const DistillArgs& a, int64_t row) { return a.weight ? a.weight[row] : 1.f; }
 
-// Rows of at most NT * NV vectors.
+// Rows of at most NT * NV vectors.  Up to 16 vectors a thread four waves share a SIMD,
+// so that one row's loads run beside another's stores.
 template <class T, int NT, int NV>
-__global__ void __launch_bounds__(NT) k_distill_held(DistillArgs a) {
+__global__ void __launch_bounds__(NT, NV > 16 ? 2 : 4) k_distill_held(DistillArgs a) {
   using RT = RowT<T>;
   constexpr int VEC = RT::VEC;
   __shared__ Shared<NT> S;
@@ -405,18 +406,22 @@ void held(const DistillArgs& a, hipStream_t s) {
 
 template <class T>
 void launch_t(const DistillArgs& a, hipStream_t s) {
-  constexpr int VEC = RowT<T>::VEC, CHUNK = 256 * 4 * VEC;
+  constexpr int VEC = RowT<T>::VEC;  // 16 bytes
+  // the smallest workgroup that holds the row: 8192 fp32 classes, 4096 rows, 55 us at 8
+  // vectors a thread, 61 at 16 half empty, 69 read twice
   if (a.C <= 64 * 4 * VEC) return held<T, 64, 4>(a, s);
   if (a.C <= 256 * 4 * VEC) return held<T, 256, 4>(a, s);
-  if (a.scratch && a.R <= 64) {
-    const Cut cut = cut_row(a.C, CHUNK, SEGS / a.R);
-    if (cut.segs > 1) {
-      hipLaunchKernelGGL((k_distill_stats<T, 256, 4>), dim3((unsigned)(a.R * cut.segs)), dim3(256), 0, s, a, cut.segs, cut.seg);
-      return segments<T, true>(a, a.grad ? cut : Cut{1, a.C}, cut.segs, s);
-    }
-  }
+  if (a.C <= 256 * 8 * VEC) return held<T, 256, 8>(a, s);
   if (a.C <= 256 * 16 * VEC) return held<T, 256, 16>(a, s);
-  if (a.C <= 1024 * 16 * VEC) return held<T, 1024, 16>(a, s);
+  if (a.C <= 512 * 16 * VEC) return held<T, 512, 16>(a, s);
+  // beyond 128 KB a row, too few rows for the chip go in segments (fp32, 131072 classes,
+  // with gradients: 8 rows 10 us against 23, 64 rows 25 against 32, 128 rows 45 against 41)
+  if (a.scratch && a.R <= 64) {
+    const Cut cut = cut_row(a.C, 256 * 4 * VEC, SEGS / a.R);
+    hipLaunchKernelGGL((k_distill_stats<T, 256, 4>), dim3((unsigned)(a.R * cut.segs)), dim3(256), 0, s, a, cut.segs, cut.seg);
+    return segments<T, true>(a, a.grad ? cut : Cut{1, a.C}, cut.segs, s);
+  }
+  if (a.C <= 512 * 32 * VEC) return held<T, 512, 32>(a, s);
   hipLaunchKernelGGL((k_distill_long<T, 1024, 4>), dim3((unsigned)std::min<int64_t>(a.R, GRID)), dim3(1024), 0, s, a);
 }
 
