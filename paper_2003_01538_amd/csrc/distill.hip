@@ -24,34 +24,6 @@ namespace fs {
 
 namespace {
 
-// Two maxima or sums over the workgroup at the price of one.
-template <int NT>
-__device__ __forceinline__ void block_max2(float& a, float& b, float (*sh)[2]) {
-  a = row_wave_max(a);
-  b = row_wave_max(b);
-  if constexpr (NT > 64) {
-    if ((threadIdx.x & 63) == 0) { sh[threadIdx.x >> 6][0] = a; sh[threadIdx.x >> 6][1] = b; }
-    __syncthreads();
-    a = sh[0][0]; b = sh[0][1];
-#pragma unroll
-    for (int w = 1; w < NT / 64; ++w) { a = fmaxf(a, sh[w][0]); b = fmaxf(b, sh[w][1]); }
-    __syncthreads();
-  }
-}
-template <int NT>
-__device__ __forceinline__ void block_sum2(float& a, float& b, float (*sh)[2]) {
-  a = row_wave_sum(a);
-  b = row_wave_sum(b);
-  if constexpr (NT > 64) {
-    if ((threadIdx.x & 63) == 0) { sh[threadIdx.x >> 6][0] = a; sh[threadIdx.x >> 6][1] = b; }
-    __syncthreads();
-    a = b = 0.f;
-#pragma unroll
-    for (int w = 0; w < NT / 64; ++w) { a += sh[w][0]; b += sh[w][1]; }
-    __syncthreads();
-  }
-}
-
 // The teacher's entries of a row, entry n NT + t with thread t, and what the
 // workgroup shares of them.
 template <int NT>
@@ -228,7 +200,7 @@ __global__ void __launch_bounds__(NT, NV > 16 ? 2 : 4) k_distill_held(DistillArg
 
 // Statistics of z[first .. end - 1] over the workgroup: m and s.
 template <class T, int NT, int NV>
-__device__ __forceinline__ RowStats<false> walk_stats(const T* z, int64_t first, int64_t end, float k2, float* sh) {
+__device__ __forceinline__ RowStats<false> walk_stats(const T* z, int64_t first, int64_t end, float k2, float (*sh)[2]) {
   using RT = RowT<T>;
   constexpr int VEC = RT::VEC, CHUNK = NT * NV * VEC;
   RowStats<false> st;
@@ -280,7 +252,7 @@ __global__ void __launch_bounds__(NT) k_distill_long(DistillArgs a) {
     const T* z = static_cast<const T*>(a.z) + row * a.ld;
     Teacher<T, NT> t;
     t.load(a, row, z);
-    const RowStats<false> rs = walk_stats<T, NT, NV>(z, 0, row_end(a.C), k2, &S.red[0][0]);
+    const RowStats<false> rs = walk_stats<T, NT, NV>(z, 0, row_end(a.C), k2, S.red);
     const Stats st = stats_of(rs.m, rs.s);
     const float us = block_sum<NT>(t.exps(block_max<NT>(t.max(), &S.red[0][0]), k2), &S.red[0][0]);
     t.share(us, S);
@@ -313,7 +285,7 @@ __device__ __forceinline__ float* scratch_z(const DistillArgs& a, int segs) {
 
 template <class T, int NT, int NV>
 __global__ void __launch_bounds__(NT) k_distill_stats(DistillArgs a, int segs, int seg) {
-  __shared__ float sh[NT / 64];
+  __shared__ float sh[NT / 64][2];
   const int row = blockIdx.x / segs, first = (blockIdx.x - row * segs) * seg;
   const T* z = static_cast<const T*>(a.z) + (int64_t)row * a.ld;
   if (first == 0)
@@ -354,7 +326,7 @@ __global__ void __launch_bounds__(NT) k_distill_segment(DistillArgs a, int segs,
 #pragma unroll
       for (int n = 0; n < Teacher<T, NT>::E; ++n)
         if (t.id[n] >= 0) t.z[n] = scratch_z(a, parts)[row * a.K + n * NT + threadIdx.x];
-      rs.over_block<NT>(k2, &S.red[0][0]);
+      rs.over_block<NT>(k2, S.red);
       st = stats_of(rs.m, rs.s);
       if (first == 0) {
         if (a.stats && threadIdx.x == 0) { a.stats[row * 2] = st.m; a.stats[row * 2 + 1] = st.l; }

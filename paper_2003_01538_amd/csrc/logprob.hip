@@ -45,7 +45,7 @@ constexpr int SLACK = 64;  // entries that the list grows by before it is cut
 template <int NT>
 struct Selection {
   static constexpr int LIST = NT == 64 ? 512 : 1024;
-  __attribute__((aligned(16))) uint64_t list[LIST];
+  __attribute__((aligned(16))) uint64_t list[LIST + 8];
   uint64_t top[MAX_TOP];
   float maxima[NT];
   int hits[3], n, count[NT / 64];
@@ -82,11 +82,14 @@ __device__ __forceinline__ void cut(Selection<NT>& S, Progress& p, int K) {
   const int n = p.n;
   for (int i = threadIdx.x; i < n; i += NT) {
     const uint64_t own = S.list[i];
-    int rank = 0, j = 0;
-    for (; j + 8 <= n; j += 8)
+    int rank = 0;
+    for (int j = 0; j < n; j += 8) {
+      uint64_t e[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) rank += S.list[j + u] > own ? 1 : 0;
-    for (; j < n; ++j) rank += S.list[j] > own ? 1 : 0;
+      for (int u = 0; u < 8; ++u) e[u] = S.list[j + u];  // up to 7 behind the last one, which do not count
+#pragma unroll
+      for (int u = 0; u < 8; ++u) rank += e[u] > own && j + u < n ? 1 : 0;
+    }
     if (rank < K) S.top[rank] = own;
   }
   __syncthreads();
@@ -98,11 +101,12 @@ __device__ __forceinline__ void cut(Selection<NT>& S, Progress& p, int K) {
 }
 
 // The largest number of which count() says at least K, searched from the highest
-// bit down; ends early once count() says at most `most`.
+// bit down; ends early once count() says at most `most`.  It lies in lo .. hi.
 template <class Count>
-__device__ __forceinline__ uint32_t search(int K, int most, Count&& count) {
-  uint32_t x = 0;
-  for (int bit = 31; bit >= 0; --bit) {
+__device__ __forceinline__ uint32_t search(uint32_t lo, uint32_t hi, int K, int most, Count&& count) {
+  const int bits = lo == hi ? 0 : 32 - __builtin_clz(lo ^ hi);  // those above are the same
+  uint32_t x = bits == 32 ? 0 : lo >> bits << bits;
+  for (int bit = bits - 1; bit >= 0; --bit) {
     const int c = count(x | 1u << bit);
     if (c < K) continue;
     x |= 1u << bit;
@@ -138,31 +142,36 @@ __device__ __forceinline__ void select_chunk(Selection<NT>& S, Progress& p, int 
     cut(S, p, K);
     // a logit that K or a few more of the threads' maxima reach, of groups of threads if those are enough
     if (hits > K) {
+      const int near = K + (K >> 3) + 2;
+      float q[NT / 64], g;  // the maxima; the largest of each group of NT / 64
       if constexpr (NT == 64) {
-        from = fmaxf(from, key_logit(search(K, K + (K >> 3) + 2, [&](uint32_t k) { return (int)__popcll(__ballot(best >= key_logit(k))); })));
+        g = q[0] = best;
       } else {
         if (turn > 0) {
           S.maxima[threadIdx.x] = best;
           __syncthreads();
         }
-        float q[NT / 64], g = -INFINITY;
+        g = -INFINITY;
 #pragma unroll
         for (int w = 0; w < NT / 64; ++w) {
           q[w] = S.maxima[w * 64 + lane];
           g = fmaxf(g, q[w]);
         }
-        uint32_t k;
-        if (K <= 40 && (int)__popcll(__ballot(g >= from)) >= K)
-          k = search(K, K + (K >> 3) + 2, [&](uint32_t k) { return (int)__popcll(__ballot(g >= key_logit(k))); });
-        else
-          k = search(K, K + (K >> 3) + 2, [&](uint32_t k) {
-            int c = 0;
-#pragma unroll
-            for (int w = 0; w < NT / 64; ++w) c += (int)__popcll(__ballot(q[w] >= key_logit(k)));
-            return c;
-          });
-        from = fmaxf(from, key_logit(k));
       }
+      const uint32_t hi = order_key(row_wave_max(g));
+      uint32_t k;
+      if (K <= 40 && (int)__popcll(__ballot(g >= from)) >= K) {
+        const uint32_t lo = order_key(-row_wave_max(g >= from ? -g : -INFINITY));
+        k = search(lo, hi, K, near, [&](uint32_t k) { return (int)__popcll(__ballot(g >= key_logit(k))); });
+      } else {
+        k = search(order_key(from), hi, K, near, [&](uint32_t k) {
+          int c = 0;
+#pragma unroll
+          for (int w = 0; w < NT / 64; ++w) c += (int)__popcll(__ballot(q[w] >= key_logit(k)));
+          return c;
+        });
+      }
+      from = fmaxf(from, key_logit(k));
     }
   }
   // list them, all of a wave's in one place; false: there is no room for them
@@ -211,9 +220,10 @@ __device__ __forceinline__ void select_chunk(Selection<NT>& S, Progress& p, int 
       }
       return block_count<NT>(n, S.count);
     };
-    const float kth = key_logit(search(K, most, [&](uint32_t k) { return reach(fmaxf(from, key_logit(k)), ~0u); }));
+    const uint32_t top = order_key(INFINITY);  // keys above are no logit's
+    const float kth = key_logit(search(order_key(from), top, K, most, [&](uint32_t k) { return k > top ? 0 : reach(fmaxf(from, key_logit(k)), ~0u); }));
     from = fmaxf(from, kth);
-    const uint32_t last = ~search(K, most, [&](uint32_t k) { return reach(from, ~k); });
+    const uint32_t last = ~search(0, ~0u, K, most, [&](uint32_t k) { return reach(from, ~k); });
     __syncthreads();
     list([&](float z, int c) { return z > from || (z == from && uint32_t(c) <= last); });
     __syncthreads();
@@ -234,14 +244,20 @@ __device__ __forceinline__ void select_begin(Selection<NT>& S) {
 }
 
 // ln p of the given classes, entropy and alternatives of a row from its statistics and its list.
+// `mine`: given_logit of this thread's first given class, loaded before the walk.
+template <class T>
+__device__ __forceinline__ float given_logit(const LogprobArgs& a, int64_t row, const T* z, int i) {
+  if (i >= a.T) return -INFINITY;
+  const int c = a.classes[row * a.T + i];
+  return c >= 0 && c < a.C ? RowT<T>::one(z + c) : -INFINITY;
+}
 template <class T, int NT>
-__device__ __forceinline__ void write_row(const LogprobArgs& a, int64_t row, const T* z, const RowStats<true>& st,
+__device__ __forceinline__ void write_row(const LogprobArgs& a, int64_t row, const T* z, float mine, const RowStats<true>& st,
                                           Selection<NT>& S, int n) {
   const float ls = logf(st.s);
   if (a.entropy && threadIdx.x == 0) a.entropy[row] = st.s == 0.f ? 0.f : ls - st.t / st.s;
   for (int i = threadIdx.x; i < a.T; i += NT) {
-    const int c = a.classes[row * a.T + i];
-    const float v = c >= 0 && c < a.C ? RowT<T>::one(z + c) : -INFINITY;
+    const float v = i < NT ? mine : given_logit(a, row, z, i);
     a.logp[row * a.T + i] = v == -INFINITY ? -INFINITY : (v - st.m) - ls;
   }
   for (int i = threadIdx.x; i < a.K; i += NT) {
@@ -262,7 +278,7 @@ __global__ void __launch_bounds__(NT) k_logprob(LogprobArgs a, int segs, int seg
   using RT = RowT<T>;
   constexpr int VEC = RT::VEC, NE = NV * VEC, CHUNK = NT * NE;
   __shared__ Selection<NT> S;
-  __shared__ float sh[NT / 64];
+  __shared__ float sh[NT / 64][2];
   const int64_t items = (int64_t)a.R * segs;
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
     const int64_t row = SPLIT ? item / segs : item;
@@ -274,6 +290,7 @@ __global__ void __launch_bounds__(NT) k_logprob(LogprobArgs a, int segs, int seg
     Progress p;
     u32x4 v[NV], next[NV];
     row_chunk<T, NT, NV>(z, first, end, v);
+    const float mine = SPLIT ? 0.f : given_logit(a, row, z, threadIdx.x);
     for (int64_t from = first; from < end; from += CHUNK) {
       const bool more = from + CHUNK < end;
       if (more) row_chunk<T, NT, NV>(z, from + CHUNK, end, next);
@@ -310,7 +327,7 @@ __global__ void __launch_bounds__(NT) k_logprob(LogprobArgs a, int segs, int seg
       if (threadIdx.x == 0) *part = Part{st.m, st.s, st.t, p.n};
       for (int i = threadIdx.x; i < a.K; i += NT) list[i] = i < p.n ? S.list[i] : 0;
     } else {
-      write_row<T, NT>(a, row, z, st, S, p.n);
+      write_row<T, NT>(a, row, z, mine, st, S, p.n);
     }
     __syncthreads();
   }
@@ -322,10 +339,12 @@ constexpr int JOIN_T = 256, JOIN_E = 8;
 template <class T>
 __global__ void __launch_bounds__(JOIN_T) k_logprob_join(LogprobArgs a, int segs) {
   __shared__ Selection<JOIN_T> S;
-  __shared__ float sh[JOIN_T / 64];
+  __shared__ float sh[JOIN_T / 64][2];
   const int64_t row = blockIdx.x;
   const Part* part = static_cast<const Part*>(a.scratch) + row * segs;
   const uint64_t* list = reinterpret_cast<const uint64_t*>(static_cast<const Part*>(a.scratch) + (int64_t)a.R * segs) + row * segs * a.K;
+  const T* z = static_cast<const T*>(a.z) + row * a.ld;
+  const float mine = given_logit(a, row, z, threadIdx.x);
   select_begin(S);
   RowStats<true> st;
   for (int i = threadIdx.x; i < segs; i += JOIN_T) {
@@ -358,34 +377,46 @@ __global__ void __launch_bounds__(JOIN_T) k_logprob_join(LogprobArgs a, int segs
   __syncthreads();
   cut(S, p, a.K);
   st.over_block<JOIN_T>(LOG2E, sh);
-  write_row<T, JOIN_T>(a, row, static_cast<const T*>(a.z) + row * a.ld, st, S, p.n);
+  write_row<T, JOIN_T>(a, row, z, mine, st, S, p.n);
+}
+
+constexpr int SEGS = 1024;  // segments of all rows that are split
+
+template <class T, int NT, int NV>
+void whole(const LogprobArgs& a, hipStream_t s) {
+  constexpr int64_t GRID = 1 << 20;  // workgroups walk the rows beyond
+  hipLaunchKernelGGL((k_logprob<T, NT, NV, false>), dim3((unsigned)std::min<int64_t>(a.R, GRID)), dim3(NT), 0, s, a, 1, a.C);
 }
 
 template <class T>
 void launch_t(const LogprobArgs& a, hipStream_t s) {
-  constexpr int64_t GRID = 1 << 20;  // workgroups walk the rows beyond
-  if (a.C <= 2048) {
-    hipLaunchKernelGGL((k_logprob<T, 64, 16 / RowT<T>::VEC, false>), dim3((unsigned)std::min<int64_t>(a.R, GRID)), dim3(64), 0, s, a, 1, a.C);
-    return;
+  constexpr int VEC = RowT<T>::VEC, NV = 16 / VEC;  // 16 logits a thread at a time: with 32 registers limit the waves (bf16, 2048 x 131072, 258 us against 190)
+  // a wave per row, as long as its 64 maxima tell the K best from the rest
+  if (a.C <= 2048 && a.K <= 40) return whole<T, 64, NV>(a, s);
+  // few long rows in segments: fp32, K = 20, 131072 classes, one row 11 us against 32, 64
+  // rows 22 against 38, 256 rows 44 against 43; 64 rows of 10000 11.5 against 10
+  constexpr int CHUNK = 256 * 16;
+  if (a.scratch && a.R < 256 && a.C > 16384) {
+    const int chunks = (a.C - 1) / CHUNK + 1, most = std::min(chunks, SEGS / a.R);
+    const int seg = (chunks - 1) / most + 1, segs = (chunks - 1) / seg + 1;
+    if (segs > 1) {
+      hipLaunchKernelGGL((k_logprob<T, 256, NV, true>), dim3((unsigned)(a.R * segs)), dim3(256), 0, s, a, segs, seg * CHUNK);
+      hipLaunchKernelGGL((k_logprob_join<T>), dim3((unsigned)a.R), dim3(JOIN_T), 0, s, a, segs);
+      return;
+    }
   }
-  constexpr int CHUNK = 256 * 4 * RowT<T>::VEC;
-  int64_t segs = 1;
-  if (a.scratch && a.R < 512) segs = std::min<int64_t>((a.C + CHUNK - 1) / CHUNK, std::max<int64_t>(1, 512 / a.R));
-  if (segs > 1) {
-    const int chunks = (a.C + CHUNK - 1) / CHUNK;
-    const int seg = (int)((chunks + segs - 1) / segs) * CHUNK;
-    segs = (a.C + seg - 1) / seg;
-    hipLaunchKernelGGL((k_logprob<T, 256, 4, true>), dim3((unsigned)(a.R * segs)), dim3(256), 0, s, a, (int)segs, seg);
-    hipLaunchKernelGGL((k_logprob_join<T>), dim3((unsigned)a.R), dim3(JOIN_T), 0, s, a, (int)segs);
-    return;
-  }
-  hipLaunchKernelGGL((k_logprob<T, 256, 4, false>), dim3((unsigned)std::min<int64_t>(a.R, GRID)), dim3(256), 0, s, a, 1, a.C);
+  // four waves per row, more when there are too few rows for the chip (fp32, K = 20, 131072
+  // classes: 256 rows 43 us with 16 waves, 54 with 8, 79 with 4; 512 rows 80, 66 and
+  // 87; 2048 rows 298, 238 and 209)
+  if (a.R < 512 && a.C > 4096) return whole<T, 1024, NV>(a, s);
+  if (a.R < 1024 && a.C > 4096) return whole<T, 512, NV>(a, s);
+  return whole<T, 256, NV>(a, s);
 }
 
 }  // namespace
 
-// At most 512 segments in all, each of a Part and K entries.
-static_assert(512 * (sizeof(Part) + MAX_TOP * 8) <= FS_ROW_SCRATCH_BYTES, "scratch");
+// A Part and K entries of each segment.
+static_assert(SEGS * (sizeof(Part) + MAX_TOP * 8) <= FS_ROW_SCRATCH_BYTES, "scratch");
 
 void launch_logprob(const LogprobArgs& a, Prec p, hipStream_t s) {
   if (p == BF16) launch_t<uint16_t>(a, s);

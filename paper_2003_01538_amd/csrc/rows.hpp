@@ -207,6 +207,34 @@ __device__ __forceinline__ float block_max(float v, float* sh) {
   return v;
 }
 
+// Two sums or maxima at the price of one.
+template <int NT>
+__device__ __forceinline__ void block_max2(float& a, float& b, float (*sh)[2]) {
+  a = row_wave_max(a);
+  b = row_wave_max(b);
+  if constexpr (NT > 64) {
+    if ((threadIdx.x & 63) == 0) { sh[threadIdx.x >> 6][0] = a; sh[threadIdx.x >> 6][1] = b; }
+    __syncthreads();
+    a = sh[0][0]; b = sh[0][1];
+#pragma unroll
+    for (int w = 1; w < NT / 64; ++w) { a = fmaxf(a, sh[w][0]); b = fmaxf(b, sh[w][1]); }
+    __syncthreads();
+  }
+}
+template <int NT>
+__device__ __forceinline__ void block_sum2(float& a, float& b, float (*sh)[2]) {
+  a = row_wave_sum(a);
+  b = row_wave_sum(b);
+  if constexpr (NT > 64) {
+    if ((threadIdx.x & 63) == 0) { sh[threadIdx.x >> 6][0] = a; sh[threadIdx.x >> 6][1] = b; }
+    __syncthreads();
+    a = b = 0.f;
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) { a += sh[w][0]; b += sh[w][1]; }
+    __syncthreads();
+  }
+}
+
 // Running statistics of the logits that a thread has seen.  k2 = log2(e) c.
 // T: whether t is wanted (c is 1 then).
 template <bool T>
@@ -225,10 +253,10 @@ struct RowStats {
     if constexpr (T) t = fmaf(e, fmaxf(d, FAR), t);
   }
   template <int NT>
-  __device__ __forceinline__ void over_block(float k2, float* sh) {
-    lift(block_max<NT>(m, sh), k2);
-    s = block_sum<NT>(s, sh);
-    if constexpr (T) t = block_sum<NT>(t, sh);
+  __device__ __forceinline__ void over_block(float k2, float (*sh)[2]) {
+    lift(block_max<NT>(m, &sh[0][0]), k2);
+    if constexpr (T) block_sum2<NT>(s, t, sh);
+    else s = block_sum<NT>(s, &sh[0][0]);
   }
 };
 

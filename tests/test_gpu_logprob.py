@@ -136,6 +136,31 @@ def test_orders_that_are_hard_for_a_selection(gpu_lib, C, kind, prec):
         Call(z, prec, 1, K).run().check()
 
 
+@pytest.mark.parametrize("prec", [BF, F])
+@pytest.mark.parametrize("C", [900, 5000, 33000, 140000])
+def test_many_infinities(gpu_lib, C, prec):
+    # more candidates than a list holds, all of them at the largest logit there is
+    inf = float("inf")
+    z = logits(4, C, 10)
+    z[0] = inf
+    z[1, ::2] = inf
+    z[2, C // 2:] = inf
+    z[3, ::3] = torch.finfo(torch.float32).max if prec == F else torch.finfo(torch.bfloat16).max
+    for K in (1, 50, 128):
+        Call(z, prec, 1, K).run().check()
+
+
+def test_wave_rows_with_many_alternatives(gpu_lib):
+    for K in (39, 40, 41, 64, 65, 128):
+        Call(logits(30, 1000, 11), F, 1, K).run().check()
+
+
+@pytest.mark.parametrize("R", [255, 256, 511, 512, 1023, 1024])
+def test_row_counts_around_the_rules(gpu_lib, R):
+    Call(logits(R, 5000, 12), F, 1, 3).run().check()
+    Call(logits(R, 16400, 12), BF, 1, 3).run().check()
+
+
 def test_large_logits_keep_their_differences(gpu_lib):
     z = logits(4, 3000, 4)
     for shift in (1000.0, -30000.0):
