@@ -48,6 +48,7 @@ struct Selection {
   __attribute__((aligned(16))) uint64_t list[LIST + 8];
   uint64_t top[MAX_TOP];
   float maxima[NT];
+  __attribute__((aligned(16))) float group[NT / 64][64];
   int hits[3], n, count[NT / 64];
 };
 
@@ -75,20 +76,23 @@ __device__ __forceinline__ int block_count(int v, int* sh) {
   return v;
 }
 
-// Cut the list to the K best, in falling order.
+// Cut the list to the K best, in falling order: an entry's place is the number of
+// those before it.  Every thread has seen p.n.
 template <int NT>
 __device__ __forceinline__ void cut(Selection<NT>& S, Progress& p, int K) {
   if (p.sorted) return;
   const int n = p.n;
+  if (threadIdx.x < 8) S.list[n + threadIdx.x] = 0;  // comes after every entry
+  __syncthreads();
   for (int i = threadIdx.x; i < n; i += NT) {
     const uint64_t own = S.list[i];
     int rank = 0;
     for (int j = 0; j < n; j += 8) {
       uint64_t e[8];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) e[u] = S.list[j + u];  // up to 7 behind the last one, which do not count
+      for (int u = 0; u < 8; ++u) e[u] = S.list[j + u];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) rank += e[u] > own && j + u < n ? 1 : 0;
+      for (int u = 0; u < 8; ++u) rank += e[u] > own ? 1 : 0;
     }
     if (rank < K) S.top[rank] = own;
   }
@@ -98,6 +102,35 @@ __device__ __forceinline__ void cut(Selection<NT>& S, Progress& p, int K) {
   if (threadIdx.x == 0) S.n = p.n;
   p.sorted = true;
   __syncthreads();
+}
+
+// The K-th largest of the 64 lanes' values, K <= 64; `sh`: the wave's own 64 floats.
+__device__ __forceinline__ float kth_of_wave(float g, int K, float* sh) {
+  sh[threadIdx.x & 63] = g;
+  int before = 0;
+#pragma unroll
+  for (int i = 0; i < 64; i += 4) {
+    const floatx4 q = *reinterpret_cast<const floatx4*>(sh + i);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) before += q[e] > g ? 1 : 0;
+  }
+  return -row_wave_max(before < K ? -g : -INFINITY);
+}
+
+// a[j] of registers, by halving with masks (as a choice of elements the compiler
+// makes it a comparison with every index for every step)
+template <int N>
+__device__ __forceinline__ uint32_t pick(const uint32_t (&a)[N], int j) {
+  uint32_t t[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) t[i] = a[i];
+#pragma unroll
+  for (int s = N / 2; s > 0; s /= 2) {
+    const uint32_t m = j & s ? ~0u : 0u;
+#pragma unroll
+    for (int i = 0; i < s; ++i) t[i] = (t[i + s] & m) | (t[i] & ~m);
+  }
+  return t[0];
 }
 
 // The largest number of which count() says at least K, searched from the highest
@@ -116,12 +149,14 @@ __device__ __forceinline__ uint32_t search(uint32_t lo, uint32_t hi, int K, int 
 }
 
 // One chunk's candidates into the list.  get(j, z, c): this thread's j-th of NE
-// logits and its class; best: the largest of them (-inf: none).
-template <int NT, int NE, class Get>
-__device__ __forceinline__ void select_chunk(Selection<NT>& S, Progress& p, int K, float best, Get&& get) {
+// logits and its class, entry_of(j) the same as an entry for a j that is not a
+// constant; best: the largest of them (-inf: none).  TIES: a logit equal to the bar may
+// be of a lower class than those before it, so it is a candidate too.
+template <int NT, int NE, bool TIES, class Get, class EntryOf>
+__device__ __forceinline__ void select_chunk(Selection<NT>& S, Progress& p, int K, float best, Get&& get, EntryOf&& entry_of) {
   constexpr int LIST = Selection<NT>::LIST;
   const int lane = threadIdx.x & 63, turn = p.turn++;
-  const uint64_t wave_hits = __ballot(best > p.bar);
+  const uint64_t wave_hits = __ballot(best > p.bar || (TIES && best == p.bar && best > -INFINITY));
   int hits;
   if constexpr (NT == 64) {
     hits = (int)__popcll(wave_hits);
@@ -135,14 +170,13 @@ __device__ __forceinline__ void select_chunk(Selection<NT>& S, Progress& p, int 
   }
   if (hits == 0) return;
 
-  // candidates: z >= from, the logit next above the bar
-  float from = key_logit(order_key(p.bar) + 1);
+  // candidates: z >= from, the bar or the logit next above it
+  float from = TIES && p.bar > -INFINITY ? p.bar : key_logit(order_key(p.bar) + 1);
   const bool many = p.n + hits * NE > LIST;
   if (many) {
     cut(S, p, K);
     // a logit that K or a few more of the threads' maxima reach, of groups of threads if those are enough
     if (hits > K) {
-      const int near = K + (K >> 3) + 2;
       float q[NT / 64], g;  // the maxima; the largest of each group of NT / 64
       if constexpr (NT == 64) {
         g = q[0] = best;
@@ -158,20 +192,17 @@ __device__ __forceinline__ void select_chunk(Selection<NT>& S, Progress& p, int 
           g = fmaxf(g, q[w]);
         }
       }
-      const uint32_t hi = order_key(row_wave_max(g));
-      uint32_t k;
       if (K <= 40 && (int)__popcll(__ballot(g >= from)) >= K) {
-        const uint32_t lo = order_key(-row_wave_max(g >= from ? -g : -INFINITY));
-        k = search(lo, hi, K, near, [&](uint32_t k) { return (int)__popcll(__ballot(g >= key_logit(k))); });
+        from = fmaxf(from, kth_of_wave(g, K, S.group[threadIdx.x >> 6]));
       } else {
-        k = search(order_key(from), hi, K, near, [&](uint32_t k) {
+        const uint32_t k = search(order_key(from), order_key(row_wave_max(g)), K, K + (K >> 3) + 2, [&](uint32_t k) {
           int c = 0;
 #pragma unroll
           for (int w = 0; w < NT / 64; ++w) c += (int)__popcll(__ballot(q[w] >= key_logit(k)));
           return c;
         });
+        from = fmaxf(from, key_logit(k));
       }
-      from = fmaxf(from, key_logit(k));
     }
   }
   // list them, all of a wave's in one place; false: there is no room for them
@@ -191,13 +222,10 @@ __device__ __forceinline__ void select_chunk(Selection<NT>& S, Progress& p, int 
     at = __builtin_amdgcn_readfirstlane(at);
     if (at + all > LIST) return;  // seen below, by every thread
     at += upto - count;
-#pragma unroll
-    for (int j = 0; j < NE; ++j)
-      if (mine >> j & 1) {
-        float z;
-        int c;
-        get(j, z, c);
-        S.list[at++] = entry(z, c);
+    while (__ballot(mine != 0))  // mostly one or two of a thread's logits
+      if (mine) {
+        S.list[at++] = entry_of(__ffs(mine) - 1);
+        mine &= mine - 1;
       }
   };
   static_assert(NE <= 32, "a bit for each logit");
@@ -230,10 +258,7 @@ __device__ __forceinline__ void select_chunk(Selection<NT>& S, Progress& p, int 
   }
   p.n = S.n;
   p.sorted = false;
-  if (p.n >= K + SLACK || many) {
-    __syncthreads();  // S.n has been read
-    cut(S, p, K);
-  }
+  if (p.n >= K + SLACK || many) cut(S, p, K);
   if (p.sorted && p.n == K) p.bar = entry_logit(S.list[K - 1]);
 }
 
@@ -306,19 +331,25 @@ __global__ void __launch_bounds__(NT) k_logprob(LogprobArgs a, int segs, int seg
         for (int e = 0; e < VEC; ++e) st.add(RT::get(v[j], e), LOG2E);
       if (a.K > 0) {
         const int base = (int)from + (int)threadIdx.x * VEC;
-        select_chunk<NT, NE>(S, p, a.K, best, [&](int j, float& x, int& c) {
+        select_chunk<NT, NE, false>(S, p, a.K, best, [&](int j, float& x, int& c) {
           int at = base;
           u32x4 raw = v[j / VEC];
           __asm__ volatile("" : "+v"(at), "+v"(raw));  // classes and fp32 logits are formed where they are used, not kept
           x = RT::get(raw, j % VEC);
           c = at + j / VEC * NT * VEC + j % VEC;
+        }, [&](int j) {
+          uint32_t words[NV * 4];
+#pragma unroll
+          for (int i = 0; i < NV * 4; ++i) words[i] = v[i / 4][i % 4];
+          const uint32_t w = pick(words, j * 4 / VEC);
+          const float x = VEC == 4 ? __uint_as_float(w) : __uint_as_float(j & 1 ? w & 0xffff0000u : w << 16);
+          return entry(x, base + j / VEC * NT * VEC + j % VEC);
         });
       }
       if (more)
 #pragma unroll
         for (int j = 0; j < NV; ++j) v[j] = next[j];
     }
-    __syncthreads();
     cut(S, p, a.K);
     st.over_block<NT>(LOG2E, sh);
     if constexpr (SPLIT) {
@@ -335,7 +366,8 @@ __global__ void __launch_bounds__(NT) k_logprob(LogprobArgs a, int segs, int seg
 
 constexpr int JOIN_T = 256, JOIN_E = 8;
 
-// The segments of a row, joined.
+// The segments of a row, joined.  The best of every segment come first, so that
+// the threads' first entries are the largest.
 template <class T>
 __global__ void __launch_bounds__(JOIN_T) k_logprob_join(LogprobArgs a, int segs) {
   __shared__ Selection<JOIN_T> S;
@@ -344,6 +376,16 @@ __global__ void __launch_bounds__(JOIN_T) k_logprob_join(LogprobArgs a, int segs
   const Part* part = static_cast<const Part*>(a.scratch) + row * segs;
   const uint64_t* list = reinterpret_cast<const uint64_t*>(static_cast<const Part*>(a.scratch) + (int64_t)a.R * segs) + row * segs * a.K;
   const T* z = static_cast<const T*>(a.z) + row * a.ld;
+  const int entries = segs * a.K;
+  uint64_t e[JOIN_E];
+  auto load = [&](int from) {
+#pragma unroll
+    for (int j = 0; j < JOIN_E; ++j) {
+      const int i = from + j * JOIN_T + threadIdx.x;
+      e[j] = i < entries ? list[(i % segs) * a.K + i / segs] : 0;
+    }
+  };
+  load(0);
   const float mine = given_logit(a, row, z, threadIdx.x);
   select_begin(S);
   RowStats<true> st;
@@ -358,23 +400,25 @@ __global__ void __launch_bounds__(JOIN_T) k_logprob_join(LogprobArgs a, int segs
     st.t += q.t;
   }
   Progress p;
-  // equal logits in later entries have higher classes, as select_chunk's bar needs: segments
-  // are in the order of their classes, and so are equal logits inside one
-  for (int from = 0; from < segs * a.K; from += JOIN_T * JOIN_E) {
-    uint64_t e[JOIN_E];
+  for (int from = 0; from < entries; from += JOIN_T * JOIN_E) {
+    if (from > 0) load(from);
     float best = -INFINITY;
 #pragma unroll
-    for (int j = 0; j < JOIN_E; ++j) {
-      const int i = from + j * JOIN_T + threadIdx.x;
-      e[j] = i < segs * a.K ? list[i] : 0;
+    for (int j = 0; j < JOIN_E; ++j)
       if (e[j]) best = fmaxf(best, entry_logit(e[j]));
-    }
-    select_chunk<JOIN_T, JOIN_E>(S, p, a.K, best, [&](int j, float& x, int& c) {
+    select_chunk<JOIN_T, JOIN_E, true>(S, p, a.K, best, [&](int j, float& x, int& c) {
       x = e[j] ? entry_logit(e[j]) : -INFINITY;
       c = entry_class(e[j]);
+    }, [&](int j) {
+      uint32_t lo[JOIN_E], hi[JOIN_E];
+#pragma unroll
+      for (int i = 0; i < JOIN_E; ++i) {
+        lo[i] = uint32_t(e[i]);
+        hi[i] = uint32_t(e[i] >> 32);
+      }
+      return uint64_t(pick(hi, j)) << 32 | pick(lo, j);
     });
   }
-  __syncthreads();
   cut(S, p, a.K);
   st.over_block<JOIN_T>(LOG2E, sh);
   write_row<T, JOIN_T>(a, row, z, mine, st, S, p.n);
