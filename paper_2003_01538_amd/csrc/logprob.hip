@@ -434,11 +434,12 @@ void whole(const LogprobArgs& a, hipStream_t s) {
 
 template <class T>
 void launch_t(const LogprobArgs& a, hipStream_t s) {
-  constexpr int VEC = RowT<T>::VEC, NV = 16 / VEC;  // 16 logits a thread at a time: with 32 registers limit the waves (bf16, 2048 x 131072, 258 us against 190)
-  // a wave per row, as long as its 64 maxima tell the K best from the rest
+  constexpr int VEC = RowT<T>::VEC, NV = 16 / VEC;  // 16 logits a thread at a time: with 32, registers limit the waves (bf16, 2048 x 131072: 258 us against 179)
+  // a wave per row, as long as its 64 maxima tell the K best from the rest (96 rows of
+  // 1000, fp32, 4.9 us at K = 5; at K = 64 four waves take 7.6 us against 64)
   if (a.C <= 2048 && a.K <= 40) return whole<T, 64, NV>(a, s);
   // few long rows in segments: fp32, K = 20, 131072 classes, one row 11 us against 32, 64
-  // rows 22 against 38, 256 rows 44 against 43; 64 rows of 10000 11.5 against 10
+  // rows 21 against 38, 256 rows 42 against 43; one row of 16384 9.9 against 8.0
   constexpr int CHUNK = 256 * 16;
   if (a.scratch && a.R < 256 && a.C > 16384) {
     const int chunks = (a.C - 1) / CHUNK + 1, most = std::min(chunks, SEGS / a.R);
@@ -449,11 +450,11 @@ void launch_t(const LogprobArgs& a, hipStream_t s) {
       return;
     }
   }
-  // four waves per row, more when there are too few rows for the chip (fp32, K = 20, 131072
-  // classes: 256 rows 43 us with 16 waves, 54 with 8, 79 with 4; 512 rows 80, 66 and
-  // 87; 2048 rows 298, 238 and 209)
-  if (a.R < 512 && a.C > 4096) return whole<T, 1024, NV>(a, s);
-  if (a.R < 1024 && a.C > 4096) return whole<T, 512, NV>(a, s);
+  // four waves per row, more when there are too few rows for the chip (fp32, K = 20: one
+  // row of 8192 8.2 us with 16 waves, 6.1 with 8, 7.9 with 4; 256 rows of 131072 44, 52 and
+  // 79; 512 rows 76, 64 and 82; 1000 rows of 10000 34, 23 and 18)
+  if (a.R < 512 && a.C > 8192) return whole<T, 1024, NV>(a, s);
+  if ((a.R < 512 && a.C > 4096) || (a.R < 1024 && a.C > 32768)) return whole<T, 512, NV>(a, s);
   return whole<T, 256, NV>(a, s);
 }
 
