@@ -95,20 +95,56 @@ __device__ __forceinline__ void load_lds(__amdgpu_buffer_rsrc_t r, char* to, uin
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)to, 16, off, 0, 0, 0);
 }
 
-__device__ __forceinline__ float activate(float v, int act) {
-  if (act == FS_ACT_RELU) return v > 0.f ? v : 0.f;
-  if (act == FS_ACT_GELU) {
-    // v Phi(v), Phi from Hastings' rational approximation of erf (Abramowitz and Stegun
-    // 7.1.26: |error| <= 1.5e-7): a third of the time of erff, which took 80 us of
-    // 305 for 4096 x 8192 outputs
-    const float x = fabsf(v) * 0.70710678f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.f));
-    const float p = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-    const float q = 0.5f * p * __builtin_amdgcn_exp2f(-1.44269504f * x * x);  // Phi(-|v|)
-    return v * (v < 0.f ? q : 1.f - q);
+// v Phi(v), Phi from Hastings' rational approximation of erf (Abramowitz and Stegun
+// 7.1.26: |error| <= 1.5e-7), a third of erff's time, which was 80 us of 305 for
+// 4096 x 8192 outputs.
+__device__ __forceinline__ float gelu(float v) {
+  const float x = fabsf(v) * 0.70710678f, t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.f));
+  const float p = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+  const float q = 0.5f * p * __builtin_amdgcn_exp2f(-1.44269504f * x * x);  // Phi(-|v|)
+  return v * (v < 0.f ? q : 1.f - q);
+}
+
+__device__ __forceinline__ floatx4 activate(floatx4 v, int act) {
+  if (act == FS_ACT_RELU) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = v[e] > 0.f ? v[e] : 0.f;
+  } else if (act == FS_ACT_GELU) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = gelu(v[e]);
+  } else if (act == FS_ACT_SILU) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = v[e] * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * v[e]));
   }
-  if (act == FS_ACT_SILU) return v * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.44269504f * v));
   return v;
 }
+
+// Bias, residual and activation, in fp32.
+__device__ __forceinline__ floatx4 epilogue(const LinearArgs& a, floatx4 v, floatx4 bias, floatx4 res) {
+  v += bias;
+  if (a.res_first) v += res;
+  v = activate(v, a.act);
+  if (a.res && !a.res_first) v += res;
+  return v;
+}
+
+// Four outputs or residuals at any element: raw as loaded, widened, narrowed and stored.
+template <bool F32> struct Out4 {
+  typedef floatx4 Raw;
+  static __device__ __forceinline__ Raw load(const void* p, int64_t o) { return *reinterpret_cast<const floatx4_at4*>(static_cast<const float*>(p) + o); }
+  static __device__ __forceinline__ floatx4 wide(Raw r) { return r; }
+  static __device__ __forceinline__ void store(void* p, int64_t o, floatx4 v) { *reinterpret_cast<floatx4_at4*>(static_cast<float*>(p) + o) = v; }
+};
+template <> struct Out4<false> {
+  typedef u32x2 Raw;
+  static __device__ __forceinline__ Raw load(const void* p, int64_t o) { return *reinterpret_cast<const u32x2_at2*>(static_cast<const uint16_t*>(p) + o); }
+  static __device__ __forceinline__ floatx4 wide(Raw q) {
+    return floatx4{__uint_as_float(q[0] << 16), __uint_as_float(q[0] & 0xffff0000u), __uint_as_float(q[1] << 16), __uint_as_float(q[1] & 0xffff0000u)};
+  }
+  static __device__ __forceinline__ void store(void* p, int64_t o, floatx4 v) {
+    *reinterpret_cast<u32x2_at2*>(static_cast<uint16_t*>(p) + o) = __builtin_bit_cast(u32x2, __builtin_convertvector(v, bf16x4));
+  }
+};
 
 // The bias of features n .. n + 3, 0 for those that do not exist.
 struct Bias4 {
@@ -132,43 +168,28 @@ __device__ __forceinline__ floatx4 residual4(const LinearArgs& a, int m, int n) 
   const int64_t o = (int64_t)m * a.ldres + n;
   const float* const f = static_cast<const float*>(a.res) + o;
   const uint16_t* const h = static_cast<const uint16_t*>(a.res) + o;
-  if (n + 4 <= a.N) {
-    if (a.out_f32) return *reinterpret_cast<const floatx4_at4*>(f);
-    const u32x2 q = *reinterpret_cast<const u32x2_at2*>(h);
-    return floatx4{__uint_as_float(q[0] << 16), __uint_as_float(q[0] & 0xffff0000u), __uint_as_float(q[1] << 16),
-                   __uint_as_float(q[1] & 0xffff0000u)};
-  }
+  if (n + 4 <= a.N) return a.out_f32 ? Out4<true>::load(a.res, o) : Out4<false>::wide(Out4<false>::load(a.res, o));
 #pragma unroll
   for (int e = 0; e < 4; ++e)
     if (n + e < a.N) r[e] = a.out_f32 ? f[e] : bf2f(h[e]);
   return r;
 }
 
-// Bias, residual, activation and the one rounding of those of outputs
-// (m, n .. n + 3) that exist.
+// Those of outputs (m, n .. n + 3) that exist, from their sums.
 __device__ __forceinline__ void finish4(const LinearArgs& a, int m, int n, floatx4 v, const Bias4& bias, floatx4 res) {
   if (m >= a.M || n >= a.N) return;
-  v += bias.v;
-  if (a.res_first) v += res;
-  if (a.act != FS_ACT_NONE) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = activate(v[e], a.act);
-  }
-  if (a.res && !a.res_first) v += res;
+  v = epilogue(a, v, bias.v, res);
   const int64_t o = (int64_t)m * a.ldy + n;
-  float* const f = static_cast<float*>(a.y) + o;
-  uint16_t* const h = static_cast<uint16_t*>(a.y) + o;
   if (n + 4 <= a.N) {
-    if (a.out_f32) *reinterpret_cast<floatx4_at4*>(f) = v;
-    else
-      *reinterpret_cast<u32x2_at2*>(h) = u32x2{f2bf(v[0]) | uint32_t(f2bf(v[1])) << 16, f2bf(v[2]) | uint32_t(f2bf(v[3])) << 16};
+    if (a.out_f32) Out4<true>::store(a.y, o, v);
+    else Out4<false>::store(a.y, o, v);
     return;
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e)
     if (n + e < a.N) {
-      if (a.out_f32) f[e] = v[e];
-      else h[e] = f2bf(v[e]);
+      if (a.out_f32) static_cast<float*>(a.y)[o + e] = v[e];
+      else static_cast<uint16_t*>(a.y)[o + e] = f2bf(v[e]);
     }
 }
 
@@ -493,14 +514,10 @@ __global__ void __launch_bounds__(WM * WN * 64) k_linear_tile(LinearArgs a) {
   constexpr int TR = NT / (BN / 4), PASSES = WM * 32 / TR;  // rows per pass
   const int n = n0 + tid % (BN / 4) * 4, r0 = tid / (BN / 4);
   const Bias4 bias(a, n);
-  for (int i = 0; i < FM; ++i) {
-    auto row = [&](int pass) {
-      const int r = pass * TR + r0;
-      return m0 + (r / 32 * FM + i) * 32 + r % 32;
-    };
-    floatx4 res[PASSES];
-#pragma unroll
-    for (int pass = 0; pass < PASSES; ++pass) res[pass] = residual4(a, row(pass), n);
+  // row of pass p in block i: m0 + 32 i + r0 + a number that p alone gives
+  static_assert(32 % TR == 0, "a pass lies in one wave row's block");
+  auto rel = [](int pass) { return pass * TR / 32 * FM * 32 + pass * TR % 32; };
+  auto put_down = [&](int i) {
     __syncthreads();
 #pragma unroll
     for (int ii = 0; ii < FM; ++ii)
@@ -512,9 +529,35 @@ __global__ void __launch_bounds__(WM * WN * 64) k_linear_tile(LinearArgs a) {
             *reinterpret_cast<floatx4*>(out + (wm * 32 + fr) * PITCH + (wn * FN + j) * 32 + 8 * g + 4 * fq) =
                 floatx4{acc[ii][j][4 * g], acc[ii][j][4 * g + 1], acc[ii][j][4 * g + 2], acc[ii][j][4 * g + 3]};
     __syncthreads();
+  };
+  auto sums = [&](int pass) { return *reinterpret_cast<const floatx4*>(out + (pass * TR + r0) * PITCH + n - n0); };
+  auto whole = [&](auto f32) {  // a tile without an edge
+    using O = Out4<f32>;
+    for (int i = 0; i < FM; ++i) {
+      const int64_t m = m0 + 32 * i + r0;
+      typename O::Raw res[PASSES];
+      if (a.res)
 #pragma unroll
-    for (int pass = 0; pass < PASSES; ++pass)
-      finish4(a, row(pass), n, *reinterpret_cast<const floatx4*>(out + (pass * TR + r0) * PITCH + n - n0), bias, res[pass]);
+        for (int pass = 0; pass < PASSES; ++pass) res[pass] = O::load(a.res, m * a.ldres + n + rel(pass) * a.ldres);
+      put_down(i);
+#pragma unroll
+      for (int pass = 0; pass < PASSES; ++pass)
+        O::store(a.y, m * a.ldy + n + rel(pass) * a.ldy,
+                 epilogue(a, sums(pass), bias.v, a.res ? O::wide(res[pass]) : floatx4{0.f, 0.f, 0.f, 0.f}));
+    }
+  };
+  if (m0 + BM <= a.M && n0 + BN <= a.N) {
+    if (a.out_f32) whole(std::true_type{});
+    else whole(std::false_type{});
+    return;
+  }
+  for (int i = 0; i < FM; ++i) {
+    put_down(i);
+#pragma unroll 1
+    for (int pass = 0; pass < PASSES; ++pass) {
+      const int m = m0 + 32 * i + r0 + rel(pass);
+      finish4(a, m, n, sums(pass), bias, residual4(a, m, n));
+    }
   }
 }
 
@@ -586,10 +629,11 @@ void launch_t(const LinearArgs& a, hipStream_t s) {
   // a tile of 256 rows is addressed by 31-bit offsets from its first one
   const bool near = (255 * std::max(a.ldx, a.ldw) + a.K) * (int64_t)sizeof(T) < (int64_t(1) << 31);
   // up to 32 rows the weights are read once, 16 features a workgroup, and time is that of
-  // reading them (4096 features, K = 25088, bf16: 37 us for one row, 5.5 TB/s; 16
-  // waves against 8: 37 against 42 us) and, at 32 rows, of every workgroup reading x (70 us)
+  // reading them (4096 features, K = 25088, bf16: 37 us for one row, 5.5 TB/s; 8
+  // waves 42) and, at 32 rows, of every workgroup reading x too (72 us, 8 waves 75:
+  // 2.4 MB a workgroup, 616 MB in all out of L2)
   if (a.M <= 16) return few<T, 1, 1, 16, 2>(a, s);
-  if (a.M <= 32) return few<T, 2, 1, 8, 4>(a, s);
+  if (a.M <= 32) return few<T, 2, 1, 16, 2>(a, s);
   switch (pick(a, F, dma, near)) {
     case FEW_32x32: return few<T, 2, 2, 8, 2>(a, s);
     case FEW_64x32: return few<T, 4, 2, 8, 1>(a, s);
