@@ -210,6 +210,23 @@ def test_rows_at_a_32_bit_offset(gpu_lib):
     assert (big[: R - 2, 1:] == big[0, 1]).all() and abs(float(big[0, 1]) * C - 1) < 128 * U
 
 
+def test_more_rows_than_workgroups(gpu_lib):
+    R, C, K = (1 << 20) + 70, 5, 2
+    z, _, u = inputs(R, C, K, seed=8)
+    ids = torch.stack([torch.arange(R, device="cuda") % C, (torch.arange(R, device="cuda") + 2) % C], 1).int().contiguous()
+    loss, stats, grad, again = (torch.empty(*s, device="cuda") for s in ((R,), (R, 2), (R, C), (R, C)))
+    head = (z.data_ptr(), C, R, C, F, ids.data_ptr(), u.data_ptr(), K, 2.0, 0)
+    fsb.fs_distill_device(*head, loss.data_ptr(), stats.data_ptr(), grad.data_ptr(), C, 0, stream())
+    fsb.fs_distill_grad_device(*head, stats.data_ptr(), again.data_ptr(), C, stream())
+    lp, q = torch.log_softmax(z.double() / 2, 1), torch.softmax(u.double() / 2, 1)
+    want = (q * (q.log() - lp.gather(1, ids.long()))).sum(1)
+    g = lp.exp().scatter_add(1, ids.long(), -q) / 2
+    # |ln p|, |ln q| up to 20 here
+    assert bool(((loss.double() - want).abs() <= (256 + 16 * 20) * U).all())
+    for got in (grad, again):
+        assert bool(((got.double() - g).abs() <= 2 * (64 + 4 * 20) * U / 2 + 4 * U * g.abs()).all())
+
+
 def test_streams_and_graphs(gpu_lib):
     s = torch.cuda.Stream()
     calls = [Call(*inputs(R, C, 8, seed=6), F) for R, C in ((2, 130000), (96, 1000), (3, 40000))]

@@ -100,7 +100,25 @@ def test_no_bias_one_residual_row_and_in_place(gpu_lib, M):
     check(x, w, None, r, r, BF, 0, 0, res=before)
 
 
-@pytest.mark.parametrize("M", [1, 70])
+@pytest.mark.parametrize("prec,out", [(BF, BF), (F, F)])
+@pytest.mark.parametrize("pad", [0, 3])
+@pytest.mark.parametrize("M,N,K", [
+    (4000, 4090, 520), (4000, 4090, 2056), (2000, 4090, 2056), (1000, 4090, 2056), (1000, 4090, 520), (500, 4090, 520), (4096, 4096, 64),
+])
+def test_many_tiles(gpu_lib, M, N, K, pad, prec, out):
+    # the tiles of 64 x 64 up to 256 x 256, most with ragged edges; the definition in 64 bits on the GPU
+    x, w, b, r, y = make(M, N, K, prec, out, True, pads=(pad, pad, pad, pad), seed=9)
+    call(x, w, b, r, y, prec, out, 1, 1)
+    xd, wd, rd = x.view.double(), w.view.double(), r.view.double()
+    want = (xd @ wd.t() + b.double() + rd).clamp_min(0)
+    size = xd.abs() @ wd.abs().t() + b.double().abs() + rd.abs()
+    half = 2.0 ** -8 if out == BF else U  # as in tolerance()
+    off = (y.view.double() - want).abs() - (1.13 * (min(2 * K, 160) + 24) * U * size + half * want.abs() + 1e-37)
+    assert bool((off <= 0).all()), (float(off.max()), int(off.argmax()) // N, int(off.argmax()) % N)
+    assert y.untouched()
+
+
+@pytest.mark.parametrize("M", [1, 70, 3000])
 def test_empty_sum_and_no_rows(gpu_lib, M):
     x, w, b, r, y = make(M, 50, 0, BF, F, True, seed=4)
     fsb.fs_linear_device(0, 0, 0, 0, b.data_ptr(), r.ptr, r.ld, y.ptr, y.ld, M, 50, 0, BF, F, 3, 1, stream())

@@ -182,6 +182,22 @@ def test_ensemble_rows_at_a_32_bit_offset(gpu_lib):
     assert (ids[: R - 2] == torch.arange(3, device="cuda")).all() and torch.allclose(ent[: R - 2], torch.tensor(math.log(C)).cuda())
 
 
+def test_more_rows_than_workgroups(gpu_lib):
+    R, C, K = (1 << 20) + 70, 5, 3
+    z = logits(R, C, 13)
+    f = lambda *s: torch.empty(*s, device="cuda")
+    cls = (torch.arange(R, device="cuda") % C).int()
+    logp, ent, best, ids = f(R), f(R), f(R, K), torch.empty(R, K, dtype=torch.int32, device="cuda")
+    fsb.fs_logprob_device(z.data_ptr(), C, R, C, F, cls.data_ptr(), 1, K, logp.data_ptr(), ent.data_ptr(), ids.data_ptr(), best.data_ptr(),
+                          0, stream())
+    lp = torch.log_softmax(z.double(), 1)
+    v, i = torch.sort(z, dim=1, descending=True, stable=True)
+    assert torch.equal(ids.long(), i[:, :K])
+    for got, want in ((logp, lp.gather(1, cls.long()[:, None])[:, 0]), (best, lp.gather(1, i[:, :K]))):
+        assert bool(((got.double() - want).abs() <= (128 + 8 * want.abs()) * U).all())
+    assert bool(((ent.double() + (lp.exp() * lp).sum(1)).abs() <= (128 + 48 * (1 + math.log(C))) * U).all())
+
+
 def test_two_streams_with_scratch_of_their_own(gpu_lib):
     a, b = torch.cuda.Stream(), torch.cuda.Stream()
     one, two = Call(logits(1, 131072, 6), F, 1, 20), Call(logits(3, 90000, 7), BF, 1, 50)
