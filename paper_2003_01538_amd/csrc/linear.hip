@@ -283,6 +283,87 @@ __global__ void __launch_bounds__(NW * 64) k_linear_few(LinearArgs a) {
   finish4(a, om, on, s, bias, res);
 }
 
+// The same for up to 64 aligned rows, where time is that of bringing x to every
+// workgroup out of L2.  Each wave brings its own steps through LDS by loads
+// that write it: those take whole 128-byte lines of 8 rows, where the loads into
+// registers take half lines of 16.  Nothing is shared between the waves, so there is no
+// barrier: a wave waits for its own loads, S steps of which are on their way.
+template <class T, int FM, int NW, int S>
+__global__ void __launch_bounds__(NW * 64) k_linear_stream(LinearArgs a) {
+  using L = LinT<T>;
+  constexpr int VEC = L::VEC, STEP = 8 * VEC, ES = sizeof(T);
+  constexpr int STAGE = (1 + FM) * 16 * ROW, LOADS = 2 * (1 + FM);  // bytes and load instructions of a step
+  static_assert(S * STAGE >= FM * 1024, "the sums fit where the steps were");
+  __shared__ __attribute__((aligned(1024))) char lds[NW * S * STAGE];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n0 = blockIdx.x * 16;
+  const int steps = (a.K + STEP - 1) / STEP;
+  char* const own = lds + wave * S * STAGE;
+
+  // load p fills rows 8 p .. of the stage (16 of w, then x), chunks as in lds_dma.hpp;
+  // rows that do not exist read the last one
+  const __amdgpu_buffer_rsrc_t rw = rsrc(static_cast<const T*>(a.w) + (int64_t)n0 * a.ldw, (uint32_t)(((min(16, a.N - n0) - 1) * a.ldw + a.K) * ES));
+  const __amdgpu_buffer_rsrc_t rx = rsrc(a.x, (uint32_t)(((a.M - 1) * a.ldx + a.K) * ES));
+  const int kc[2] = {((lane & 7) ^ swz(lane >> 3)) * VEC, ((lane & 7) ^ swz(8 + (lane >> 3))) * VEC};
+  uint32_t off[LOADS];
+#pragma unroll
+  for (int p = 0; p < LOADS; ++p) {
+    const int r = p * 8 + (lane >> 3);
+    off[p] = (uint32_t)(((p < 2 ? min(r, a.N - n0 - 1) * a.ldw : min(r - 16, a.M - 1) * a.ldx) + kc[p & 1]) * ES);
+  }
+  auto fetch = [&](int s, int stage) {  // zeros behind the end, by the same number of loads
+    const uint32_t kb[2] = {s * STEP + kc[0] < a.K ? (uint32_t)(s * STEP * ES) : OOB, s * STEP + kc[1] < a.K ? (uint32_t)(s * STEP * ES) : OOB};
+#pragma unroll
+    for (int p = 0; p < LOADS; ++p) load_lds(p < 2 ? rw : rx, own + stage * STAGE + p * 1024, off[p] + kb[p & 1]);
+  };
+
+  const int om = wave * 16 + (lane & 15), on = n0 + (lane >> 4) * 4;
+  const bool finishes = wave < FM;
+  const Bias4 bias(a, finishes ? on : a.N);
+  const floatx4 res = residual4(a, finishes ? om : a.M, on);
+  __builtin_amdgcn_sched_barrier(0);
+
+  floatx4 acc[FM];
+#pragma unroll
+  for (int i = 0; i < FM; ++i) acc[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int t = 0; t < S; ++t) fetch(wave + t * NW, t);
+  int stage = 0;
+  for (int s = wave; s < steps; s += NW) {
+    wait_vmcnt<(S - 1) * LOADS>();
+    __asm__ __volatile__("" ::: "memory");
+    const char* at = own + stage * STAGE + (lane & 15) * ROW;
+    u32x4 w[2], x[FM][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int c = ((4 * h + (lane >> 4)) ^ swz(lane & 15)) << 4;
+      w[h] = *reinterpret_cast<const u32x4*>(at + c);
+#pragma unroll
+      for (int i = 0; i < FM; ++i) x[i][h] = *reinterpret_cast<const u32x4*>(at + (1 + i) * 16 * ROW + c);
+    }
+    __asm__ __volatile__("" ::: "memory");
+    wait_lgkm0();  // the operands are in registers: the stage may be filled again
+    __asm__ __volatile__("" ::: "memory");
+    fetch(s + S * NW, stage);
+    stage = stage + 1 == S ? 0 : stage + 1;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < FM; ++i) acc[i] = L::mma16(w[h], x[i][h], acc[i]);
+  }
+  wait_vmcnt<0>();
+  __syncthreads();
+  floatx4* const part = reinterpret_cast<floatx4*>(lds);
+#pragma unroll
+  for (int i = 0; i < FM; ++i) part[(wave * FM + i) * 64 + lane] = acc[i];
+  __syncthreads();
+  if (!finishes) return;
+  floatx4 s = part[wave * 64 + lane];
+#pragma unroll
+  for (int q = 1; q < NW; ++q) s += part[(q * FM + wave) * 64 + lane];
+  finish4(a, om, on, s, bias, res);
+}
+
 // -------------------------------------------------------------- many tiles
 // A tile of BM rows x BN features on WM x WN waves.  K-tiles of 128 bytes a row
 // lie in LDS as in lds_dma.hpp, NBUF of them in turn.  DMA: the loads write LDS
@@ -567,13 +648,18 @@ void few(const LinearArgs& a, hipStream_t s) {
   hipLaunchKernelGGL((k_linear_few<T, FM, FN, NW, U>), dim3((unsigned)tiles), dim3(NW * 64), 0, s, a);
 }
 
+template <class T, int FM, int NW, int S>
+void stream(const LinearArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((k_linear_stream<T, FM, NW, S>), dim3((unsigned)((a.N + 15) / 16)), dim3(NW * 64), 0, s, a);
+}
+
 template <class T, int BM, int BN, int WM, int WN, bool DMA, int NBUF>
 void tile(const LinearArgs& a, hipStream_t s) {
   const int64_t tiles = (int64_t)((a.N + BN - 1) / BN) * ((a.M + BM - 1) / BM);
   hipLaunchKernelGGL((k_linear_tile<T, BM, BN, WM, WN, DMA, NBUF>), dim3((unsigned)tiles), dim3(WM * WN * 64), 0, s, a);
 }
 
-// The kernels of more than 32 rows, and what a K-tile (128 bytes of a row) costs
+// The other kernels, and what a K-tile (128 bytes of a row) costs
 // one workgroup of each, in us: one / `fit` of them on a CU, measured at 128 to 4096
 // rows, 4096 features and K = 4096, and what a round of workgroups costs besides.
 // One row per kernel, by type and by how the loads go.
@@ -598,7 +684,7 @@ constexpr Cost COSTS[2][2][KERNELS] = {
 // rest.  (bf16, K = 4096: 512 x 4096 outputs 64 x 128 32 us against 36 for 64 x 64 and
 // 44 for 128 x 128; 1024 x 4096 128 x 128 45 against 66 and, 256 x 256, 86; 2048 x 4096
 // 256 x 128 69 against 75 and 91; 4096 x 4096 256 x 256 114 against 134 for 256 x 128.)
-Kernel pick(const LinearArgs& a, bool f32, bool dma, bool near) {
+Kernel pick(const LinearArgs& a, bool f32, bool dma, bool near, double* us) {
   const int64_t steps = ((int64_t)a.K * (f32 ? 4 : 2) + ROW - 1) / ROW;
   Kernel best = FEW_32x32;
   double least = 0;
@@ -616,7 +702,17 @@ Kernel pick(const LinearArgs& a, bool f32, bool dma, bool near) {
       best = Kernel(k);
     }
   }
+  *us = least;
   return best;
+}
+
+// What k_linear_stream takes for blocks of 16 rows, in us: a workgroup brings 47 GB/s
+// from L2 (12 TB/s in all), the chip 5.5 TB/s of weights from memory.  (4096 features, K
+// = 4096, bf16: 16 rows 9.1 us, k_linear_few 10.1; 32 rows 10.9 and 14.3; 48 rows 12.7
+// and 17.5; 64 rows 14.3 and 18.3.  K = 25088: 32 rows 51 and 72, 64 rows 71 and 93.)
+double stream_us(const LinearArgs& a, int blocks, int es) {
+  const double step = (double)a.K * es;
+  return 2. + std::max(((a.N + 15) / 16 + 255) / 256 * (16. + 16. * blocks) * step / 47e3, a.N * step / 5.5e6);
 }
 
 template <class T>
@@ -628,13 +724,23 @@ void launch_t(const LinearArgs& a, hipStream_t s) {
                    reinterpret_cast<uintptr_t>(a.w) % 16 == 0;
   // a tile of 256 rows is addressed by 31-bit offsets from its first one
   const bool near = (255 * std::max(a.ldx, a.ldw) + a.K) * (int64_t)sizeof(T) < (int64_t(1) << 31);
-  // up to 32 rows the weights are read once, 16 features a workgroup, and time is that of
-  // reading them (4096 features, K = 25088, bf16: 37 us for one row, 5.5 TB/s; 8
-  // waves 42) and, at 32 rows, of every workgroup reading x too (72 us, 8 waves 75:
-  // 2.4 MB a workgroup, 616 MB in all out of L2)
-  if (a.M <= 16) return few<T, 1, 1, 16, 2>(a, s);
-  if (a.M <= 32) return few<T, 2, 1, 16, 2>(a, s);
-  switch (pick(a, F, dma, near)) {
+  // up to 8 rows the weights are all there is to read: 16 features a workgroup (4096
+  // features, K = 25088, bf16: 37 us for one row, 5.5 TB/s; with 8 waves 42)
+  if (a.M <= 8 || (a.M <= 16 && !(dma && near))) return few<T, 1, 1, 16, 2>(a, s);
+  double us;
+  const Kernel k = pick(a, F, dma, near, &us);
+  if (a.M <= 64 && dma && near) {
+    const int blocks = (a.M + 15) / 16;
+    if (stream_us(a, blocks, sizeof(T)) < us) {
+      if (blocks == 1) return stream<T, 1, 8, 3>(a, s);
+      if (blocks == 2) return stream<T, 2, 8, 2>(a, s);
+      if (blocks == 3) return stream<T, 3, 6, 3>(a, s);
+      return stream<T, 4, 4, 3>(a, s);
+    }
+  } else if (a.M <= 32) {
+    return few<T, 2, 1, 16, 2>(a, s);
+  }
+  switch (k) {
     case FEW_32x32: return few<T, 2, 2, 8, 2>(a, s);
     case FEW_64x32: return few<T, 4, 2, 8, 1>(a, s);
     case TILE_64x64: return dma ? tile<T, 64, 64, 1, 2, true, 4>(a, s) : tile<T, 64, 64, 2, 2, false, 2>(a, s);

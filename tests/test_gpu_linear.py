@@ -65,10 +65,18 @@ def test_sizes(gpu_lib, M, N, K, prec, out):
     check(x, w, b, r, y, out, 0, 0)
 
 
+@pytest.mark.parametrize("prec", [BF, F])
+@pytest.mark.parametrize("M,N,K", [(17, 100, 4096), (32, 1000, 2048), (31, 16, 25088), (20, 33, 1032), (25, 48, 520), (32, 65, 8200)])
+def test_few_rows_over_a_long_reduction(gpu_lib, M, N, K, prec):
+    x, w, b, r, y = make(M, N, K, prec, prec, True, pads=(0, 8, 0, 0), seed=10)
+    call(x, w, b, r, y, prec, prec, 3, 0)
+    check(x, w, b, r, y, prec, 3, 0)
+
+
 @pytest.mark.parametrize("prec,out", [(BF, BF), (BF, F), (F, F)])
 @pytest.mark.parametrize("act", [0, 1, 2, 3])
 @pytest.mark.parametrize("res,first", [(0, 0), (1, 0), (1, 1)])
-@pytest.mark.parametrize("M,N,K", [(4, 72, 96), (150, 200, 128), (40, 77, 33)])
+@pytest.mark.parametrize("M,N,K", [(4, 72, 96), (150, 200, 128), (40, 77, 33), (50, 72, 96)])
 def test_epilogues(gpu_lib, M, N, K, prec, out, act, res, first):
     x, w, b, r, y = make(M, N, K, prec, out, res, seed=1)
     call(x, w, b, r, y, prec, out, act, first)
@@ -104,9 +112,10 @@ def test_no_bias_one_residual_row_and_in_place(gpu_lib, M):
 @pytest.mark.parametrize("pad", [0, 3])
 @pytest.mark.parametrize("M,N,K", [
     (4000, 4090, 520), (4000, 4090, 2056), (2000, 4090, 2056), (1000, 4090, 2056), (1000, 4090, 520), (500, 4090, 520), (4096, 4096, 64),
+    (514, 1061, 128), (135, 2834, 2264), (509, 1679, 2916), (486, 2707, 40),
 ])
 def test_many_tiles(gpu_lib, M, N, K, pad, prec, out):
-    # the tiles of 64 x 64 up to 256 x 256, most with ragged edges; the definition in 64 bits on the GPU
+    # the tiles of 64 x 32 up to 256 x 256, most with ragged edges; the definition in 64 bits on the GPU
     x, w, b, r, y = make(M, N, K, prec, out, True, pads=(pad, pad, pad, pad), seed=9)
     call(x, w, b, r, y, prec, out, 1, 1)
     xd, wd, rd = x.view.double(), w.view.double(), r.view.double()
