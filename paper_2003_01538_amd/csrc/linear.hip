@@ -336,7 +336,9 @@ __global__ void __launch_bounds__(NW * 64) k_linear_stream(LinearArgs a) {
     u32x4 w[2], x[FM][2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int c = ((4 * h + (lane >> 4)) ^ swz(lane & 15)) << 4;
+      // lane groups 0, 1, 2, 3 take chunks 0, 2, 1, 3: the groups that LDS serves together
+      // then differ in the lowest bit, and no two of their rows meet in a bank
+      const int c = ((4 * h + ((lane >> 4 & 1) << 1 | lane >> 5)) ^ swz(lane & 15)) << 4;
       w[h] = *reinterpret_cast<const u32x4*>(at + c);
 #pragma unroll
       for (int i = 0; i < FM; ++i) x[i][h] = *reinterpret_cast<const u32x4*>(at + (1 + i) * 16 * ROW + c);
