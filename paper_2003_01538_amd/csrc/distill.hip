@@ -49,6 +49,11 @@ struct Teacher {
 #pragma unroll
     for (int n = 0; n < E; ++n) z[n] = id[n] >= 0 && zr ? RowT<T>::one(zr + id[n]) : -INFINITY;
   }
+  // the student's logits have arrived: what lies there may be overwritten
+  __device__ __forceinline__ void settle() {
+#pragma unroll
+    for (int n = 0; n < E; ++n) __asm__ volatile("" : "+v"(z[n]));
+  }
   __device__ __forceinline__ float max() const {
     float m = -FLT_MAX;
 #pragma unroll
@@ -189,6 +194,7 @@ __global__ void __launch_bounds__(NT, NV > 16 ? 2 : 4) k_distill_held(DistillArg
     if (a.grad) {
       T* g = static_cast<T*>(a.grad) + row * a.ldg;
       const Grad gr(st, c, weight_of(a, row), us != 0.f);
+      t.settle();
       __syncthreads();  // the row and its teacher's classes have been read (the gradient may lie over them)
       put_chunk<T, NT, NV>(g, 0, row_end(C), v, gr);
       __syncthreads();
@@ -264,6 +270,7 @@ __global__ void __launch_bounds__(NT) k_distill_long(DistillArgs a) {
     if (a.grad) {
       T* g = static_cast<T*>(a.grad) + row * a.ldg;
       const Grad gr(st, c, weight_of(a, row), us != 0.f);
+      t.settle();
       __syncthreads();
       walk_grad<T, NT, NV>(z, g, 0, row_end(a.C), gr);
       __syncthreads();
@@ -341,6 +348,7 @@ __global__ void __launch_bounds__(NT) k_distill_segment(DistillArgs a, int segs,
     if (a.grad) {
       T* g = static_cast<T*>(a.grad) + row * a.ldg;
       const Grad gr(st, c, weight_of(a, row), us != 0.f);
+      t.settle();
       __syncthreads();  // this segment's classes of the teacher have been read
       walk_grad<T, NT, NV>(z, g, first, end, gr);
       __syncthreads();

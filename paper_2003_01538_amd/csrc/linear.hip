@@ -1,14 +1,21 @@
 // Matrix product with bias, activation and residual on a caller's tensors:
 // y[m][n] = act(sum_k x[m][k] w[n][k] + bias[n] (+ res)) (+ res).
 //
-// Two kernels.  k_linear_few is for outputs of few tiles: a workgroup makes a
+// Three kernels.  k_linear_few is for outputs of few tiles: a workgroup makes a
 // small tile and its waves split the reduction, each loading its operands
 // straight into registers (nothing is shared, so nothing is staged), and their
-// sums meet in LDS in wave order.  k_linear_tile is for many tiles: operands go
-// through LDS, each wave sums its part of the tile over the whole reduction.
+// sums meet in LDS in wave order.  k_linear_stream is its form for up to 64 aligned
+// rows.  k_linear_tile is for many tiles: operands go through LDS, each wave sums
+// its part of the tile over the whole reduction.  Rows may lie at any distance and
+// alignment; which kernel runs, with which tile, is a rule on sizes and alignment
+// (launch_t).
 //
-// Both take rows at any distance and alignment; which of them and with which
-// tile runs is a rule on sizes and alignment (launch_linear).
+// What bounds them: up to 16 rows the weights' way from memory (4096 features, K =
+// 25088, bf16, one row 37 us, 5.5 TB/s); up to 64 rows that of x from L2 to every
+// workgroup (32 rows 51 us, 12 TB/s); bf16 products of 4096 x 8192 x 4096 the power
+// that the matrix cores may take (216 to 222 us, 1.24 to 1.27 PFLOP/s, with their pipes
+// busy 73 % of the time at 1.7 GHz; the vendor's library 180 us; 240 us with GELU and
+// residual); fp32 products the matrix cores' rate (4096^3 953 us, 144 TFLOP/s).
 //
 // MFMA operands: A = weights, B = x, so that a lane's accumulators hold
 // consecutive features n of one row m.  The order of k inside a 16-byte piece
@@ -401,7 +408,7 @@ __global__ void __launch_bounds__(WM * WN * 64) k_linear_tile(LinearArgs a) {
   const __amdgpu_buffer_rsrc_t rx = rsrc(xb, DMA ? (uint32_t)(((min(BM, a.M - m0) - 1) * a.ldx + a.K) * ES) : 0u);
   const __amdgpu_buffer_rsrc_t rw = rsrc(wb, DMA ? (uint32_t)(((min(BN, a.N - n0) - 1) * a.ldw + a.K) * ES) : 0u);
   uint32_t off[PA + PB];  // bytes from the tile's first row
-  u32x4 reg[DMA ? 1 : PA + PB];
+  u32x4 reg[PA + PB];    // not DMA: a K-tile on its way
 #pragma unroll
   for (int p = 0; p < PA + PB; ++p) {
     // rows that do not exist read the last one: they enter only outputs that do not exist
@@ -411,31 +418,23 @@ __global__ void __launch_bounds__(WM * WN * 64) k_linear_tile(LinearArgs a) {
   // the offset of K-tile s; behind the reduction's end out of range: zeros, by the same number of loads
   auto tile_off = [&](int s) { return s * KT + kc < a.K ? (uint32_t)(s * KT * ES) : OOB; };
   auto fetch_piece = [&](auto p, uint32_t kb, int at) {  // at: a buffer's offset
-    if constexpr (DMA) {
-      load_lds(p < PA ? rx : rw, lds + at + (p * NT + wave * 64) * 16, off[p] + kb);
-    }
+    load_lds(p < PA ? rx : rw, lds + at + (p * NT + wave * 64) * 16, off[p] + kb);
   };
-  auto fetch = [&](int s, int buf) {
+  // K-tile s into registers, and from there into a buffer
+  auto fetch = [&](int s) {
     const int k0 = s * KT;
-    if constexpr (DMA) {
-      const uint32_t kb = tile_off(s);
-      static_for<0, PA + PB>([&](auto p) { fetch_piece(p, kb, buf * BUF); });
+    auto row = [&](int p) { return reinterpret_cast<const T*>(reinterpret_cast<const char*>(p < PA ? xb : wb) + off[p]); };
+    if (k0 + KT <= a.K) {  // the same for the whole workgroup
+#pragma unroll
+      for (int p = 0; p < PA + PB; ++p) reg[p] = full_piece(row(p), k0 + kc);
     } else {
-      auto row = [&](int p) { return reinterpret_cast<const T*>(reinterpret_cast<const char*>(p < PA ? xb : wb) + off[p]); };
-      if (k0 + KT <= a.K) {  // the same for the whole workgroup
 #pragma unroll
-        for (int p = 0; p < PA + PB; ++p) reg[p] = full_piece(row(p), k0 + kc);
-      } else {
-#pragma unroll
-        for (int p = 0; p < PA + PB; ++p) reg[p] = piece(row(p), k0 + kc, a.K);
-      }
+      for (int p = 0; p < PA + PB; ++p) reg[p] = piece(row(p), k0 + kc, a.K);
     }
   };
-  auto store = [&](int buf) {
-    if constexpr (!DMA) {
+  auto store = [&](int at) {
 #pragma unroll
-      for (int p = 0; p < PA + PB; ++p) *reinterpret_cast<u32x4*>(lds + buf * BUF + (p * NT + tid) * 16) = reg[p];
-    }
+    for (int p = 0; p < PA + PB; ++p) *reinterpret_cast<u32x4*>(lds + at + (p * NT + tid) * 16) = reg[p];
   };
 
   floatx16 acc[FM][FN];
@@ -458,14 +457,17 @@ __global__ void __launch_bounds__(WM * WN * 64) k_linear_tile(LinearArgs a) {
     wg_barrier();
   };
 
-  if constexpr (DMA && FM % 2 == 0) {
+  static_assert(DMA ? FM % 2 == 0 : NBUF == 2, "two halves, or two buffers");
+  if constexpr (DMA) {
     // Two halves per K-tile, of the upper and the lower half of the wave's row blocks.
     // The first runs on x0 and w, the second on x1 and w; during the first x1 is
     // read, during the second the next K-tile's x0 and w (a step's w once its MFMAs
     // have it).  So LDS is free for K-tile s + NBUF early, x0 and w when the first half
     // begins, x1 when the second does, and every load has NBUF - 1/2 K-tiles of time.
     // A half waits for the loads whose operands are read in it, all but the LATE issued
-    // last, after its first step, whose operands are in registers by then.  Reads and loads are issued between MFMAs, in their shadow.
+    // last, after its first step, whose operands are in registers by then.  Reads and
+    // loads are issued between MFMAs, in their shadow (all of a half's before its MFMAs:
+    // 272 us against 224 for 4096 x 8192 x 4096).
     constexpr int H = FM / 2, PH = H * 32 / (NT / 8);  // row blocks of a half; its pieces per wave row
     static_assert(H * 32 % (NT / 8) == 0 && PA == 2 * WM * PH, "pieces and halves");
     constexpr int N_LOW = PA / 2, N_UP = PA / 2 + PB, N_ALL = PA + PB;
@@ -548,11 +550,11 @@ __global__ void __launch_bounds__(WM * WN * 64) k_linear_tile(LinearArgs a) {
     // A step's operands are read during the step before it; the barrier between two
     // K-tiles lies before the last step, whose operands are in registers by then.
     u32x4 xf[2][FM], wf[2][FN];
-    auto read = [&](int buf, int ks, int set) {
+    auto read = [&](int at, int ks, int set) {
 #pragma unroll
-      for (int i = 0; i < FM; ++i) xf[set][i] = operand(A, buf * BUF, ks, i);
+      for (int i = 0; i < FM; ++i) xf[set][i] = operand(A, at, ks, i);
 #pragma unroll
-      for (int j = 0; j < FN; ++j) wf[set][j] = operand(B, buf * BUF, ks, j);
+      for (int j = 0; j < FN; ++j) wf[set][j] = operand(B, at, ks, j);
     };
     auto mma = [&](int set) {
 #pragma unroll
@@ -560,29 +562,25 @@ __global__ void __launch_bounds__(WM * WN * 64) k_linear_tile(LinearArgs a) {
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = L::mma32(wf[set][j], xf[set][i], acc[i][j]);
     };
-    fetch(0, 0);
+    fetch(0);
     store(0);
-    if constexpr (DMA) wait_vmcnt<0>();
     meet();
-    if (DMA && steps > 1) fetch(1, 1);
     read(0, 0, 0);
     for (int s = 0; s < steps; ++s) {
-      const int buf = s & 1;
+      const int at = (s & 1) * BUF;
       const bool more = s + 1 < steps;
-      if (!DMA && more) fetch(s + 1, buf ^ 1);
+      if (more) fetch(s + 1);
 #pragma unroll
       for (int ks = 0; ks < 3; ++ks) {
-        read(buf, ks + 1, (ks + 1) & 1);
+        read(at, ks + 1, (ks + 1) & 1);
         __builtin_amdgcn_sched_barrier(0);  // the reads are under way before the MFMAs
         mma(ks & 1);
         __builtin_amdgcn_sched_barrier(0);
       }
       if (more) {
-        store(buf ^ 1);
-        if constexpr (DMA) wait_vmcnt<0>();  // this wave's part of the next K-tile is in LDS
-        meet();                              // every wave's is, and all are done with this one
-        if (DMA && s + 2 < steps) fetch(s + 2, buf);
-        read(buf ^ 1, 0, 0);
+        store(at ^ BUF);
+        meet();  // every wave's part of the next K-tile is in LDS, and all are done with this one
+        read(at ^ BUF, 0, 0);
         __builtin_amdgcn_sched_barrier(0);
       }
       mma(1);

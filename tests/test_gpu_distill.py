@@ -210,6 +210,19 @@ def test_rows_at_a_32_bit_offset(gpu_lib):
     assert (big[: R - 2, 1:] == big[0, 1]).all() and abs(float(big[0, 1]) * C - 1) < 128 * U
 
 
+@pytest.mark.parametrize("R,C", [(3, 900), (2, 5000), (3, 70000), (70, 70000)])
+def test_outputs_that_are_not_asked_for(gpu_lib, R, C):
+    c = Call(*inputs(R, C, 5, seed=9), F)
+    c.run()
+    loss, stats, grad = (torch.full_like(t.view, t.mark()) for t in (c.loss, c.stats, c.grad))
+    sc = c.scratch.data_ptr()
+    fsb.fs_distill_device(*c.head(), loss.data_ptr(), 0, 0, c.grad.ld, sc, stream())
+    fsb.fs_distill_device(*c.head(), 0, stats.data_ptr(), 0, c.grad.ld, sc, stream())
+    fsb.fs_distill_device(*c.head(), 0, 0, grad.data_ptr(), C, sc, stream())
+    for got, want in ((loss, c.loss), (stats, c.stats), (grad, c.grad)):
+        assert torch.equal(got, want.view)
+
+
 def test_more_rows_than_workgroups(gpu_lib):
     R, C, K = (1 << 20) + 70, 5, 2
     z, _, u = inputs(R, C, K, seed=8)

@@ -127,6 +127,25 @@ def test_many_tiles(gpu_lib, M, N, K, pad, prec, out):
     assert y.untouched()
 
 
+@pytest.mark.parametrize("M,N,K", [(20, 64, 512), (600, 1024, 64), (4096, 4096, 64)])
+def test_one_residual_row_and_in_place_on_every_kind_of_tile(gpu_lib, M, N, K):
+    x, w, b, r, y = make(M, N, K, BF, BF, True, seed=11)
+    product = x.view.double() @ w.view.double().t()
+    size = x.view.double().abs() @ w.view.double().abs().t()
+
+    def near(res, got):
+        want = product + res
+        off = (got.double() - want).abs() - (1.13 * (min(2 * K, 160) + 24) * U * (size + res.abs()) + 2.0 ** -8 * want.abs())  # as in tolerance()
+        assert bool((off <= 0).all()), float(off.max())
+
+    call(x, w, None, r, y, BF, BF, 0, 1, ldres=0)
+    near(r.view[:1].double(), y.view)
+    before = r.view.double().clone()
+    call(x, w, None, r, r, BF, BF, 0, 0)
+    near(before, r.view)
+    assert r.untouched()
+
+
 @pytest.mark.parametrize("M", [1, 70, 3000])
 def test_empty_sum_and_no_rows(gpu_lib, M):
     x, w, b, r, y = make(M, 50, 0, BF, F, True, seed=4)
@@ -157,7 +176,7 @@ def test_not_finite_values_stay_in_their_rows(gpu_lib, M, N, K, prec):
     fine[:, 2] = False
     with np.errstate(invalid="ignore"):
         want, size = ref.linear(x.numpy(), w.numpy(), b.cpu().numpy())
-    assert (np.abs(got - want)[fine] <= tolerance(want, size, K, F)[fine]).all()
+    assert (np.abs(got[fine] - want[fine]) <= tolerance(want, size, K, F)[fine]).all()
 
 
 def test_activations_at_their_ends(gpu_lib):
@@ -170,7 +189,7 @@ def test_activations_at_their_ends(gpu_lib):
             want = ref.activation(b.cpu().numpy().astype(np.float64), act)
         got = y.numpy()[0].astype(np.float64)
         ok = np.isfinite(want)
-        assert (np.abs(got - want)[ok] <= 32 * U * np.abs(want)[ok] + 1e-6).all(), (act, got, want)
+        assert (np.abs(got[ok] - want[ok]) <= 32 * U * np.abs(want[ok]) + 1e-6).all(), (act, got, want)
         assert got[-1] == np.inf
 
 

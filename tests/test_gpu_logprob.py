@@ -182,6 +182,19 @@ def test_ensemble_rows_at_a_32_bit_offset(gpu_lib):
     assert (ids[: R - 2] == torch.arange(3, device="cuda")).all() and torch.allclose(ent[: R - 2], torch.tensor(math.log(C)).cuda())
 
 
+@pytest.mark.parametrize("R,C", [(3, 900), (2, 5000), (3, 70000)])
+def test_outputs_that_are_not_asked_for(gpu_lib, R, C):
+    full = Call(logits(R, C, 14), F, 2, 7).run()
+    z, sc = full.z, full.scratch.data_ptr()
+    logp, ent, best, ids = (torch.full_like(t.view, t.mark()) for t in (full.logp, full.entropy, full.best, full.ids))
+    head = (z.ptr, z.ld, R, C, F)
+    fsb.fs_logprob_device(*head, full.classes.data_ptr(), 2, 0, logp.data_ptr(), 0, 0, 0, sc, stream())
+    fsb.fs_logprob_device(*head, 0, 0, 7, 0, 0, ids.data_ptr(), best.data_ptr(), sc, stream())
+    fsb.fs_logprob_device(*head, 0, 0, 0, 0, ent.data_ptr(), 0, 0, sc, stream())
+    for got, want in ((logp, full.logp), (ent, full.entropy), (best, full.best), (ids, full.ids)):
+        assert torch.equal(got, want.view)
+
+
 def test_more_rows_than_workgroups(gpu_lib):
     R, C, K = (1 << 20) + 70, 5, 3
     z = logits(R, C, 13)
