@@ -495,7 +495,8 @@ fs_status fs_linear_device(const void *d_x, int64_t ldx, const void *d_w, int64_
  * A row of nothing else has entropy 0.  NaN or +inf in a row makes its ln p and
  * entropy NaN (-inf where the logit is -inf or the class does not exist);
  * NaN is never an alternative.
- * FS_ERR_INVALID for NULL, bad sizes, or when nothing is asked for. */
+ * FS_ERR_INVALID for NULL, bad sizes, or when nothing is asked for;
+ * FS_ERR_UNSUPPORTED for T beyond 2^30. */
 fs_status fs_logprob_device(const void *d_logits, int64_t ld, int32_t R, int32_t C, int32_t precision,
                             const int32_t *d_classes, int32_t T, int32_t K, float *d_logp, float *d_entropy,
                             int32_t *d_top_ids, float *d_top_logp, void *d_scratch, void *stream);

@@ -754,8 +754,24 @@ void launch_t(const LinearArgs& a, hipStream_t s) {
 }  // namespace
 
 void launch_linear(const LinearArgs& a, Prec p, hipStream_t s) {
-  if (p == BF16) launch_t<uint16_t>(a, s);
-  else launch_t<float>(a, s);
+  // A launch has fewer than 2^32 threads, of which k_linear_few gives 64 to a feature or
+  // one to two outputs: products beyond go in slices.
+  constexpr int FEATURES = 1 << 24;
+  const int64_t rows = (int64_t(1) << 32) / std::min(a.N, FEATURES) / 256 * 256;
+  const int64_t ei = p == BF16 ? 2 : 4, eo = a.out_f32 ? 4 : 2;
+  for (int64_t n = 0; n < a.N; n += FEATURES)
+    for (int64_t m = 0; m < a.M; m += rows) {
+      LinearArgs b = a;
+      b.x = static_cast<const char*>(a.x) + m * a.ldx * ei;
+      b.w = static_cast<const char*>(a.w) + n * a.ldw * ei;
+      if (a.bias) b.bias = a.bias + n;
+      if (a.res) b.res = static_cast<const char*>(a.res) + (m * a.ldres + n) * eo;
+      b.y = static_cast<char*>(a.y) + (m * a.ldy + n) * eo;
+      b.M = (int)std::min<int64_t>(rows, a.M - m);
+      b.N = (int)std::min<int64_t>(FEATURES, a.N - n);
+      if (p == BF16) launch_t<uint16_t>(b, s);
+      else launch_t<float>(b, s);
+    }
 }
 
 }  // namespace fs

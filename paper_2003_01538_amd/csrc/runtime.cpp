@@ -1768,6 +1768,7 @@ fs_status fs_logprob_device(const void* d_logits, int64_t ld, int32_t R, int32_t
     check_precision(precision);
     check_rows(d_logits, ld, R, C);
     if (T < 0) fail(FS_ERR_INVALID, "T must be >= 0");
+    if (T > 1 << 30) fail(FS_ERR_UNSUPPORTED, "T up to 2^30");
     if (K < 0 || K > FS_MAX_TOP) fail(FS_ERR_INVALID, "K must be in 0..FS_MAX_TOP");
     if (T == 0 && K == 0 && !d_entropy) fail(FS_ERR_INVALID, "no output is asked for");
     if (R == 0) return;

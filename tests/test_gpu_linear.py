@@ -252,3 +252,15 @@ def test_rows_beyond_32_bit_offsets(gpu_lib):
         want, size = ref.linear(x.float().cpu().numpy(), w.float().cpu().numpy())
         assert (np.abs(y.numpy() - want) <= tolerance(want, size, 64, F)).all()
         del big, v
+
+
+@pytest.mark.parametrize("M,N", [(1, 1 << 26), (12, (1 << 24) + 5), (1 << 26, 65)])
+def test_more_outputs_than_a_launch_has_threads(gpu_lib, M, N):
+    # one product per output: exact in fp32, rounded once
+    x, w, b, r, y = make(M, N, 1, BF, BF, M <= 12, seed=12)
+    call(x, w, b, r, y, BF, BF, 0, 0)
+    for m in range(0, M, 1 << 24):
+        rows = slice(m, m + (1 << 24))
+        want = x.view[rows].float() * w.view.float().t() + b
+        assert torch.equal(y.view[rows], (want if r is None else want + r.view.float()).bfloat16()), m
+    assert bool((y.buf[-64:] == MARK).all())

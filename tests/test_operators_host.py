@@ -52,6 +52,10 @@ def test_logprob_refuses(change, want):
     assert status(fsb.fs_logprob_device, LGP, **change) == want
 
 
+def test_logprob_refuses_more_classes_asked_for_than_it_counts():
+    assert status(fsb.fs_logprob_device, LGP, T=(1 << 30) + 1) == UNS
+
+
 @pytest.mark.parametrize("fn,base", [(fsb.fs_distill_device, DST), (fsb.fs_distill_grad_device, GRD)])
 @pytest.mark.parametrize("change,want", [
     (dict(z=None), INV), (dict(R=-1), INV), (dict(C=0), INV), (dict(ld=9), INV), (dict(prec=3), INV), (dict(K=0), INV),
