@@ -443,10 +443,12 @@ void launch_t(const LogprobArgs& a, hipStream_t s) {
   // a wave per row, as long as its 64 maxima tell the K best from the rest (96 rows of
   // 1000, fp32, 4.9 us at K = 5; at K = 64 four waves take 7.6 us against 64)
   if (a.C <= 2048 && a.K <= 40) return whole<T, 64, NV>(a, s);
-  // few long rows in segments: fp32, K = 20, 131072 classes, one row 11 us against 32, 64
-  // rows 21 against 38, 256 rows 42 against 43; one row of 16384 9.9 against 8.0
+  // few long rows in segments, down to the numbers of rows where whole ones take as long
+  // (fp32, K = 20: one row of 131072 classes 10.7 us against 29.4, 61 rows 21 against 35, 200
+  // rows 38 against 39; of 32000 10.4 against 11.7, 61 rows 12.9 against 13.1, 128 rows 15.1
+  // against 14.0; one row of 16384 9.9 against 8.0)
   constexpr int CHUNK = 256 * 16;
-  if (a.scratch && a.R < 256 && a.C > 16384) {
+  if (a.scratch && a.C > 16384 && a.R < (a.C > 32768 ? 200 : 100)) {
     const int chunks = (a.C - 1) / CHUNK + 1, most = std::min(chunks, SEGS / a.R);
     const int seg = (chunks - 1) / most + 1, segs = (chunks - 1) / seg + 1;
     if (segs > 1) {

@@ -258,3 +258,9 @@ def test_same_bits_every_time(gpu_lib):
         c.run()
         seen.append((c.entropy.view.clone(), c.best.view.clone(), c.ids.view.clone()))
     assert all(torch.equal(a, b) for s in seen[1:] for a, b in zip(s, seen[0]))
+
+
+@pytest.mark.parametrize("prec", [BF, F])
+@pytest.mark.parametrize("R,C", [(99, 17000), (100, 17000), (199, 33000), (200, 33000)])
+def test_row_counts_around_the_split(gpu_lib, R, C, prec):
+    Call(logits(R, C, 13), prec, 2, 20).run().check()
