@@ -125,14 +125,14 @@ struct Grad {
 };
 
 // The vectors that row_chunk loads, as gradients.
-template <class T, int NT, int NV>
+template <class T, int NT, int NV, bool ONCE>
 __device__ __forceinline__ void put_chunk(T* g, int64_t from, int64_t end, const u32x4 (&v)[NV], const Grad& gr) {
   constexpr int VEC = RowT<T>::VEC;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const int64_t i = from + (int64_t)(j * NT + (int)threadIdx.x) * VEC;
     const u32x4 q = gr.template vec<T>(v[j]);
-    if (from + (int64_t)(j + 1) * NT * VEC <= end) RowT<T>::store(g + i, q);  // the same for the whole workgroup
+    if (from + (int64_t)(j + 1) * NT * VEC <= end) store_vec<ONCE>(g + i, q);  // the same for the whole workgroup
     else put_vec(g, i, end, q);
   }
 }
@@ -157,7 +157,7 @@ __device__ __forceinline__ float weight_of(const DistillArgs& a, int64_t row) { 
 
 // Rows of at most NT * NV vectors.  Up to 16 vectors a thread four waves share a SIMD,
 // so that one row's loads run beside another's stores.
-template <class T, int NT, int NV>
+template <class T, int NT, int NV, bool ONCE>
 __global__ void __launch_bounds__(NT, NV > 16 ? 2 : 4) k_distill_held(DistillArgs a) {
   using RT = RowT<T>;
   constexpr int VEC = RT::VEC;
@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(NT, NV > 16 ? 2 : 4) k_distill_held(DistillArg
     const T* z = static_cast<const T*>(a.z) + row * a.ld;
     const int C = row_end(a.C);
     u32x4 v[NV];
-    row_chunk<T, NT, NV>(z, 0, C, v);
+    row_chunk<T, NT, NV, ONCE>(z, 0, C, v);
     Teacher<T, NT> t;
     t.load(a, row, z);
     float m = -FLT_MAX, um = t.max();
@@ -196,7 +196,7 @@ __global__ void __launch_bounds__(NT, NV > 16 ? 2 : 4) k_distill_held(DistillArg
       const Grad gr(st, c, weight_of(a, row), us != 0.f);
       t.settle();
       __syncthreads();  // the row and its teacher's classes have been read (the gradient may lie over them)
-      put_chunk<T, NT, NV>(g, 0, row_end(C), v, gr);
+      put_chunk<T, NT, NV, ONCE>(g, 0, row_end(C), v, gr);
       __syncthreads();
       if (us != 0.f) put_teacher<T, NT>(a, g, t, S, st, gr, c, 0, a.C);
     }
@@ -211,10 +211,10 @@ __device__ __forceinline__ RowStats<false> walk_stats(const T* z, int64_t first,
   constexpr int VEC = RT::VEC, CHUNK = NT * NV * VEC;
   RowStats<false> st;
   u32x4 v[NV], next[NV];
-  row_chunk<T, NT, NV>(z, first, end, v);
+  row_chunk<T, NT, NV, false>(z, first, end, v);
   for (int64_t from = first; from < end; from += CHUNK) {
     const bool more = from + CHUNK < end;
-    if (more) row_chunk<T, NT, NV>(z, from + CHUNK, end, next);
+    if (more) row_chunk<T, NT, NV, false>(z, from + CHUNK, end, next);
     float best = -INFINITY;
 #pragma unroll
     for (int j = 0; j < NV; ++j)
@@ -234,15 +234,15 @@ __device__ __forceinline__ RowStats<false> walk_stats(const T* z, int64_t first,
 }
 
 // The gradient without the teacher, of z[first .. end - 1].
-template <class T, int NT, int NV>
+template <class T, int NT, int NV, bool ONCE>
 __device__ __forceinline__ void walk_grad(const T* z, T* g, int64_t first, int64_t end, const Grad& gr) {
   constexpr int CHUNK = NT * NV * RowT<T>::VEC;
   u32x4 v[NV], next[NV];
-  row_chunk<T, NT, NV>(z, first, end, v);
+  row_chunk<T, NT, NV, ONCE>(z, first, end, v);
   for (int64_t from = first; from < end; from += CHUNK) {
     const bool more = from + CHUNK < end;
-    if (more) row_chunk<T, NT, NV>(z, from + CHUNK, end, next);
-    put_chunk<T, NT, NV>(g, from, end, v, gr);
+    if (more) row_chunk<T, NT, NV, ONCE>(z, from + CHUNK, end, next);
+    put_chunk<T, NT, NV, ONCE>(g, from, end, v, gr);
     if (more)
 #pragma unroll
       for (int j = 0; j < NV; ++j) v[j] = next[j];
@@ -272,7 +272,7 @@ __global__ void __launch_bounds__(NT) k_distill_long(DistillArgs a) {
       const Grad gr(st, c, weight_of(a, row), us != 0.f);
       t.settle();
       __syncthreads();
-      walk_grad<T, NT, NV>(z, g, 0, row_end(a.C), gr);
+      walk_grad<T, NT, NV, false>(z, g, 0, row_end(a.C), gr);
       __syncthreads();
       if (us != 0.f) put_teacher<T, NT>(a, g, t, S, st, gr, c, 0, a.C);
     }
@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(NT) k_distill_stats(DistillArgs a, int segs, i
 
 // Loss (the first segment's workgroup) and gradient of a segment.  PARTS: the
 // statistics are `parts` parts in the scratch memory; otherwise a.stats holds them.
-template <class T, int NT, int NV, bool PARTS>
+template <class T, int NT, int NV, bool PARTS, bool ONCE>
 __global__ void __launch_bounds__(NT) k_distill_segment(DistillArgs a, int segs, int seg, int parts) {
   __shared__ Shared<NT> S;
   const float c = 1.f / a.temperature, k2 = LOG2E * c;
@@ -350,7 +350,7 @@ __global__ void __launch_bounds__(NT) k_distill_segment(DistillArgs a, int segs,
       const Grad gr(st, c, weight_of(a, row), us != 0.f);
       t.settle();
       __syncthreads();  // this segment's classes of the teacher have been read
-      walk_grad<T, NT, NV>(z, g, first, end, gr);
+      walk_grad<T, NT, NV, ONCE>(z, g, first, end, gr);
       __syncthreads();
       if (us != 0.f) put_teacher<T, NT>(a, g, t, S, st, gr, c, first, end);
     }
@@ -373,15 +373,15 @@ Cut cut_row(int C, int chunk, int64_t want) {
   return {(chunks + per - 1) / per, per * chunk};
 }
 
-template <class T, bool PARTS>
+template <class T, bool PARTS, bool ONCE>
 void segments(const DistillArgs& a, Cut cut, int parts, hipStream_t s) {
   const int64_t items = (int64_t)a.R * cut.segs;
-  hipLaunchKernelGGL((k_distill_segment<T, 256, 4, PARTS>), dim3((unsigned)std::min(items, GRID)), dim3(256), 0, s, a, cut.segs, cut.seg, parts);
+  hipLaunchKernelGGL((k_distill_segment<T, 256, 4, PARTS, ONCE>), dim3((unsigned)std::min(items, GRID)), dim3(256), 0, s, a, cut.segs, cut.seg, parts);
 }
 
-template <class T, int NT, int NV>
+template <class T, int NT, int NV, bool ONCE>
 void held(const DistillArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((k_distill_held<T, NT, NV>), dim3((unsigned)std::min<int64_t>(a.R, GRID)), dim3(NT), 0, s, a);
+  hipLaunchKernelGGL((k_distill_held<T, NT, NV, ONCE>), dim3((unsigned)std::min<int64_t>(a.R, GRID)), dim3(NT), 0, s, a);
 }
 
 template <class T>
@@ -389,26 +389,29 @@ void launch_t(const DistillArgs& a, hipStream_t s) {
   constexpr int VEC = RowT<T>::VEC;  // 16 bytes
   // the smallest workgroup that holds the row: 8192 fp32 classes, 4096 rows, 55 us at 8
   // vectors a thread, 61 at 16 half empty, 69 read twice
-  if (a.C <= 64 * 4 * VEC) return held<T, 64, 4>(a, s);
-  if (a.C <= 256 * 4 * VEC) return held<T, 256, 4>(a, s);
-  if (a.C <= 256 * 8 * VEC) return held<T, 256, 8>(a, s);
-  if (a.C <= 256 * 16 * VEC) return held<T, 256, 16>(a, s);
-  if (a.C <= 512 * 16 * VEC) return held<T, 512, 16>(a, s);
+  if (a.C <= 64 * 4 * VEC) return held<T, 64, 4, false>(a, s);
+  if (a.C <= 256 * 4 * VEC) return held<T, 256, 4, false>(a, s);
+  const bool once = beyond_cache((int64_t)a.R * a.C * (int)sizeof(T) * (a.grad ? 2 : 1));
+  if (a.C <= 256 * 8 * VEC) return once ? held<T, 256, 8, true>(a, s) : held<T, 256, 8, false>(a, s);
+  if (a.C <= 256 * 16 * VEC) return once ? held<T, 256, 16, true>(a, s) : held<T, 256, 16, false>(a, s);
+  if (a.C <= 512 * 16 * VEC) return once ? held<T, 512, 16, true>(a, s) : held<T, 512, 16, false>(a, s);
   // beyond 128 KB a row, too few rows for the chip go in segments (fp32, 131072 classes,
   // with gradients: 8 rows 10 us against 23, 64 rows 25 against 32, 128 rows 45 against 41)
   if (a.scratch && a.R <= 64) {
     const Cut cut = cut_row(a.C, 256 * 4 * VEC, SEGS / a.R);
     hipLaunchKernelGGL((k_distill_stats<T, 256, 4>), dim3((unsigned)(a.R * cut.segs)), dim3(256), 0, s, a, cut.segs, cut.seg);
-    return segments<T, true>(a, a.grad ? cut : Cut{1, a.C}, cut.segs, s);
+    return segments<T, true, false>(a, a.grad ? cut : Cut{1, a.C}, cut.segs, s);
   }
-  if (a.C <= 512 * 32 * VEC) return held<T, 512, 32>(a, s);
+  if (a.C <= 512 * 32 * VEC) return once ? held<T, 512, 32, true>(a, s) : held<T, 512, 32, false>(a, s);
   hipLaunchKernelGGL((k_distill_long<T, 1024, 4>), dim3((unsigned)std::min<int64_t>(a.R, GRID)), dim3(1024), 0, s, a);
 }
 
 template <class T>
 void launch_grad_t(const DistillArgs& a, hipStream_t s) {
   constexpr int CHUNK = 256 * 4 * RowT<T>::VEC;
-  segments<T, false>(a, cut_row(a.C, CHUNK, std::max<int64_t>(1, 4096 / a.R)), 0, s);
+  const Cut cut = cut_row(a.C, CHUNK, std::max<int64_t>(1, 4096 / a.R));
+  if (beyond_cache((int64_t)a.R * a.C * (int)sizeof(T) * 2)) segments<T, false, true>(a, cut, 0, s);
+  else segments<T, false, false>(a, cut, 0, s);
 }
 
 }  // namespace

@@ -303,7 +303,7 @@ struct Part {
 };
 
 // Row blockIdx / segs, segment blockIdx % segs of `seg` classes; SPLIT: to the scratch memory.
-template <class T, int NT, int NV, bool SPLIT>
+template <class T, int NT, int NV, bool SPLIT, bool ONCE>
 __global__ void __launch_bounds__(NT) k_logprob(LogprobArgs a, int segs, int seg) {
   using RT = RowT<T>;
   constexpr int VEC = RT::VEC, NE = NV * VEC, CHUNK = NT * NE;
@@ -319,11 +319,11 @@ __global__ void __launch_bounds__(NT) k_logprob(LogprobArgs a, int segs, int seg
     RowStats<true> st;
     Progress p;
     u32x4 v[NV], next[NV];
-    row_chunk<T, NT, NV>(z, first, end, v);
+    row_chunk<T, NT, NV, ONCE>(z, first, end, v);
     const float mine = SPLIT ? 0.f : given_logit(a, row, z, threadIdx.x);
     for (int64_t from = first; from < end; from += CHUNK) {
       const bool more = from + CHUNK < end;
-      if (more) row_chunk<T, NT, NV>(z, from + CHUNK, end, next);
+      if (more) row_chunk<T, NT, NV, ONCE>(z, from + CHUNK, end, next);
       float best = -INFINITY;
 #pragma unroll
       for (int j = 0; j < NV; ++j)
@@ -431,10 +431,10 @@ __global__ void __launch_bounds__(JOIN_T) k_logprob_join(LogprobArgs a, int segs
 
 constexpr int SEGS = 1024;  // segments of all rows that are split
 
-template <class T, int NT, int NV>
+template <class T, int NT, int NV, bool ONCE = false>
 void whole(const LogprobArgs& a, hipStream_t s) {
   constexpr int64_t GRID = 1 << 20;  // workgroups walk the rows beyond
-  hipLaunchKernelGGL((k_logprob<T, NT, NV, false>), dim3((unsigned)std::min<int64_t>(a.R, GRID)), dim3(NT), 0, s, a, 1, a.C);
+  hipLaunchKernelGGL((k_logprob<T, NT, NV, false, ONCE>), dim3((unsigned)std::min<int64_t>(a.R, GRID)), dim3(NT), 0, s, a, 1, a.C);
 }
 
 template <class T>
@@ -452,7 +452,7 @@ void launch_t(const LogprobArgs& a, hipStream_t s) {
     const int chunks = (a.C - 1) / CHUNK + 1, most = std::min(chunks, SEGS / a.R);
     const int seg = (chunks - 1) / most + 1, segs = (chunks - 1) / seg + 1;
     if (segs > 1) {
-      hipLaunchKernelGGL((k_logprob<T, 256, NV, true>), dim3((unsigned)(a.R * segs)), dim3(256), 0, s, a, segs, seg * CHUNK);
+      hipLaunchKernelGGL((k_logprob<T, 256, NV, true, false>), dim3((unsigned)(a.R * segs)), dim3(256), 0, s, a, segs, seg * CHUNK);
       hipLaunchKernelGGL((k_logprob_join<T>), dim3((unsigned)a.R), dim3(JOIN_T), 0, s, a, segs);
       return;
     }
@@ -462,6 +462,9 @@ void launch_t(const LogprobArgs& a, hipStream_t s) {
   // 79; 512 rows 76, 64 and 82; 1000 rows of 10000 34, 23 and 18)
   if (a.R < 512 && a.C > 8192) return whole<T, 1024, NV>(a, s);
   if ((a.R < 512 && a.C > 4096) || (a.R < 1024 && a.C > 32768)) return whole<T, 512, NV>(a, s);
+  // more than the last-level cache holds is not kept there: 2048 x 131072 fp32 204 us
+  // against 197
+  if (beyond_cache((int64_t)a.R * a.C * sizeof(T))) return whole<T, 256, NV, true>(a, s);
   return whole<T, 256, NV>(a, s);
 }
 

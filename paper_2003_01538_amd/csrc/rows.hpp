@@ -32,8 +32,7 @@ typedef uint32_t u32_at2 __attribute__((aligned(2)));
 template <class T> struct RowT;
 template <> struct RowT<float> {
   static constexpr int VEC = 4;
-  static __device__ __forceinline__ u32x4 load(const float* p) { return *reinterpret_cast<const u32x4_at4*>(p); }
-  static __device__ __forceinline__ void store(float* p, u32x4 v) { *reinterpret_cast<u32x4_at4*>(p) = v; }
+  typedef u32x4_at4 Vec;
   static __device__ __forceinline__ float get(u32x4 v, int e) { return __uint_as_float(v[e]); }
   static __device__ __forceinline__ float one(const float* p) { return *p; }
   static __device__ __forceinline__ void put(float* p, float v) { *p = v; }
@@ -43,8 +42,7 @@ template <> struct RowT<float> {
 };
 template <> struct RowT<uint16_t> {  // bf16
   static constexpr int VEC = 8;
-  static __device__ __forceinline__ u32x4 load(const uint16_t* p) { return *reinterpret_cast<const u32x4_at2*>(p); }
-  static __device__ __forceinline__ void store(uint16_t* p, u32x4 v) { *reinterpret_cast<u32x4_at2*>(p) = v; }
+  typedef u32x4_at2 Vec;
   static __device__ __forceinline__ float get(u32x4 v, int e) {
     return __uint_as_float(e & 1 ? v[e >> 1] & 0xffff0000u : v[e >> 1] << 16);
   }
@@ -56,12 +54,29 @@ template <> struct RowT<uint16_t> {  // bf16
   }
 };
 
+// Whether a call that moves so many bytes gains by keeping none of them in a cache:
+// twice the last-level cache and more.
+inline bool beyond_cache(int64_t bytes) { return bytes > int64_t(400) << 20; }
+
+// A vector of a row.  ONCE: no cache is to keep it.
+template <bool ONCE, class T>
+__device__ __forceinline__ u32x4 load_vec(const T* p) {
+  const auto* v = reinterpret_cast<const typename RowT<T>::Vec*>(p);
+  return ONCE ? __builtin_nontemporal_load(v) : *v;
+}
+template <bool ONCE, class T>
+__device__ __forceinline__ void store_vec(T* p, u32x4 v) {
+  auto* to = reinterpret_cast<typename RowT<T>::Vec*>(p);
+  if (ONCE) __builtin_nontemporal_store(v, to);
+  else *to = v;
+}
+
 // Elements i .. i + VEC - 1 of a row that ends at `end`; -inf behind the end.  A
 // row's last vector is put together from pieces of 4, 2 and 1 elements, the last first.
 template <class T>
 __device__ __forceinline__ u32x4 row_vec(const T* z, int64_t i, int64_t end) {
   constexpr int VEC = RowT<T>::VEC;
-  if (i + VEC <= end) return RowT<T>::load(z + i);
+  if (i + VEC <= end) return load_vec<false>(z + i);
   const int r = (int)(end > i ? end - i : 0);
   const T* p = z + i;
   if constexpr (VEC == 8) {
@@ -98,7 +113,7 @@ template <class T>
 __device__ __forceinline__ void put_vec(T* g, int64_t i, int64_t end, u32x4 v) {
   constexpr int VEC = RowT<T>::VEC;
   if (i + VEC <= end) {
-    RowT<T>::store(g + i, v);
+    store_vec<false>(g + i, v);
     return;
   }
   const int r = (int)(end > i ? end - i : 0);
@@ -115,13 +130,13 @@ __device__ __forceinline__ void put_vec(T* g, int64_t i, int64_t end, u32x4 v) {
 
 // NV vectors of a workgroup's chunk of NT * NV vectors that begins at `from`:
 // thread t holds vectors t, t + NT, ...
-template <class T, int NT, int NV>
+template <class T, int NT, int NV, bool ONCE>
 __device__ __forceinline__ void row_chunk(const T* z, int64_t from, int64_t end, u32x4 (&v)[NV]) {
   constexpr int VEC = RowT<T>::VEC;
 #pragma unroll
   for (int j = 0; j < NV; ++j) {
     const int64_t i = from + (int64_t)(j * NT + (int)threadIdx.x) * VEC;
-    if (from + (int64_t)(j + 1) * NT * VEC <= end) v[j] = RowT<T>::load(z + i);  // the same for the whole workgroup
+    if (from + (int64_t)(j + 1) * NT * VEC <= end) v[j] = load_vec<ONCE>(z + i);  // the same for the whole workgroup
     else v[j] = row_vec(z, i, end);
   }
 }
