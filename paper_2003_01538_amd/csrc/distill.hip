@@ -373,45 +373,61 @@ Cut cut_row(int C, int chunk, int64_t want) {
   return {(chunks + per - 1) / per, per * chunk};
 }
 
-template <class T, bool PARTS, bool ONCE>
+template <class T, int NT, bool PARTS, bool ONCE>
 void segments(const DistillArgs& a, Cut cut, int parts, hipStream_t s) {
   const int64_t items = (int64_t)a.R * cut.segs;
-  hipLaunchKernelGGL((k_distill_segment<T, 256, 4, PARTS, ONCE>), dim3((unsigned)std::min(items, GRID)), dim3(256), 0, s, a, cut.segs, cut.seg, parts);
+  hipLaunchKernelGGL((k_distill_segment<T, NT, 4, PARTS, ONCE>), dim3((unsigned)std::min(items, GRID)), dim3(NT), 0, s, a, cut.segs, cut.seg, parts);
 }
 
-template <class T, int NT, int NV, bool ONCE>
-void held(const DistillArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((k_distill_held<T, NT, NV, ONCE>), dim3((unsigned)std::min<int64_t>(a.R, GRID)), dim3(NT), 0, s, a);
+// Rows in the registers of NT threads, by the first of so many vectors each that holds them.
+template <class T, int NT, bool ONCE, int NV, int... MORE>
+bool held(const DistillArgs& a, hipStream_t s) {
+  if (a.C <= NT * NV * RowT<T>::VEC) {
+    hipLaunchKernelGGL((k_distill_held<T, NT, NV, ONCE>), dim3((unsigned)std::min<int64_t>(a.R, GRID)), dim3(NT), 0, s, a);
+    return true;
+  }
+  if constexpr (sizeof...(MORE) > 0) return held<T, NT, ONCE, MORE...>(a, s);
+  return false;
 }
 
 template <class T>
 void launch_t(const DistillArgs& a, hipStream_t s) {
   constexpr int VEC = RowT<T>::VEC;  // 16 bytes
-  // the smallest workgroup that holds the row: 8192 fp32 classes, 4096 rows, 55 us at 8
-  // vectors a thread, 61 at 16 half empty, 69 read twice
-  if (a.C <= 64 * 4 * VEC) return held<T, 64, 4, false>(a, s);
-  if (a.C <= 256 * 4 * VEC) return held<T, 256, 4, false>(a, s);
+  // the fewest threads and vectors that hold the row, since places without a class cost as
+  // much as others (bf16 with gradients: 60000 rows of 2500 classes 155 us with 128 x 4
+  // vectors against 280 with 256 x 4; 8000 rows of 17000 101 with 256 x 10, 131 with 256 x
+  // 16; 4000 of 34000 112 with 512 x 10, 159 with 512 x 16); read twice, 4096 rows of 8192
+  // fp32 take 69 us against 55
+  if (held<T, 64, false, 4>(a, s) || held<T, 128, false, 4, 6>(a, s) || held<T, 256, false, 4>(a, s)) return;
   const bool once = beyond_cache((int64_t)a.R * a.C * (int)sizeof(T) * (a.grad ? 2 : 1));
-  if (a.C <= 256 * 8 * VEC) return once ? held<T, 256, 8, true>(a, s) : held<T, 256, 8, false>(a, s);
-  if (a.C <= 256 * 16 * VEC) return once ? held<T, 256, 16, true>(a, s) : held<T, 256, 16, false>(a, s);
-  if (a.C <= 512 * 16 * VEC) return once ? held<T, 512, 16, true>(a, s) : held<T, 512, 16, false>(a, s);
+  if (once ? held<T, 256, true, 6, 8, 10, 12, 14, 16>(a, s) : held<T, 256, false, 6, 8, 10, 12, 14, 16>(a, s)) return;
+  if (once ? held<T, 512, true, 10, 12, 14, 16>(a, s) : held<T, 512, false, 10, 12, 14, 16>(a, s)) return;
   // beyond 128 KB a row, too few rows for the chip go in segments (fp32, 131072 classes,
   // with gradients: 8 rows 10 us against 23, 64 rows 25 against 32, 128 rows 45 against 41)
   if (a.scratch && a.R <= 64) {
     const Cut cut = cut_row(a.C, 256 * 4 * VEC, SEGS / a.R);
     hipLaunchKernelGGL((k_distill_stats<T, 256, 4>), dim3((unsigned)(a.R * cut.segs)), dim3(256), 0, s, a, cut.segs, cut.seg);
-    return segments<T, true, false>(a, a.grad ? cut : Cut{1, a.C}, cut.segs, s);
+    return segments<T, 256, true, false>(a, a.grad ? cut : Cut{1, a.C}, cut.segs, s);
   }
-  if (a.C <= 512 * 32 * VEC) return once ? held<T, 512, 32, true>(a, s) : held<T, 512, 32, false>(a, s);
+  if (once ? held<T, 512, true, 20, 24, 28, 32>(a, s) : held<T, 512, false, 20, 24, 28, 32>(a, s)) return;
   hipLaunchKernelGGL((k_distill_long<T, 1024, 4>), dim3((unsigned)std::min<int64_t>(a.R, GRID)), dim3(1024), 0, s, a);
 }
 
+// About 4096 segments of whole chunks, the chunk by the row's length: 120000 rows of
+// 1001 fp32 205 us with one wave a row, 460 with four; 60000 rows of 2049 193 with two
+// waves, 248 with four; 8000 rows of 16384 200 with two, 184 with four.
+template <class T, int NT, bool ONCE>
+void grad_segments(const DistillArgs& a, hipStream_t s) {
+  segments<T, NT, false, ONCE>(a, cut_row(a.C, NT * 4 * RowT<T>::VEC, std::max<int64_t>(1, 4096 / a.R)), 0, s);
+}
 template <class T>
 void launch_grad_t(const DistillArgs& a, hipStream_t s) {
-  constexpr int CHUNK = 256 * 4 * RowT<T>::VEC;
-  const Cut cut = cut_row(a.C, CHUNK, std::max<int64_t>(1, 4096 / a.R));
-  if (beyond_cache((int64_t)a.R * a.C * (int)sizeof(T) * 2)) segments<T, false, true>(a, cut, 0, s);
-  else segments<T, false, false>(a, cut, 0, s);
+  constexpr int VEC = RowT<T>::VEC;
+  if (a.C <= 64 * 4 * VEC) return grad_segments<T, 64, false>(a, s);
+  const bool once = beyond_cache((int64_t)a.R * a.C * (int)sizeof(T) * 2);
+  if (a.C <= 64 * 8 * VEC) return once ? grad_segments<T, 64, true>(a, s) : grad_segments<T, 64, false>(a, s);
+  if (a.C <= 512 * 4 * VEC) return once ? grad_segments<T, 128, true>(a, s) : grad_segments<T, 128, false>(a, s);
+  return once ? grad_segments<T, 256, true>(a, s) : grad_segments<T, 256, false>(a, s);
 }
 
 }  // namespace
