@@ -221,10 +221,12 @@ __device__ __forceinline__ RowStats<false> walk_stats(const T* z, int64_t first,
 #pragma unroll
       for (int e = 0; e < VEC; ++e) best = fmaxf(best, RT::get(v[j], e));
     if (best > st.m) st.lift(best, k2);
+    RowStats<false> part = st.empty();
 #pragma unroll
     for (int j = 0; j < NV; ++j)
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) st.add(RT::get(v[j], e), k2);
+      for (int e = 0; e < VEC; ++e) part.add(RT::get(v[j], e), k2);
+    st.join(part);
     if (more)
 #pragma unroll
       for (int j = 0; j < NV; ++j) v[j] = next[j];

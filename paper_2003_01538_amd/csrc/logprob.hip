@@ -13,7 +13,7 @@
 // i-th chunk), so that the selection costs little more than the comparison with the
 // thread's maximum, which the statistics need anyway.  In a chunk with too many
 // candidates to list (the first one; rising rows) a logit that K of the threads'
-// maxima reach bounds them: for K <= 40 the K-th of 64 groups' maxima, found by
+// maxima reach bounds them: for K <= 40 (and in a wave's own rows) the K-th of 64 groups' maxima, found by
 // counting, else one found bit by bit over all of them.  Only if that leaves too
 // many, one between the chunk's K-th and LIST-th best is searched bit by bit.
 //
@@ -177,11 +177,11 @@ __device__ __forceinline__ void select_chunk(Selection<NT>& S, Progress& p, int 
 
   // candidates: z >= from, the bar or the logit next above it
   float from = TIES && p.bar > -INFINITY ? p.bar : key_logit(order_key(p.bar) + 1);
-  const bool many = p.n + hits * NE > LIST;
+  const bool many = p.n + hits * NE > LIST || (NT == 64 && hits > K);  // a wave finds a threshold in less time than it ranks a long list
   if (many) {
     cut(S, p, K);
     // a logit that K or a few more of the threads' maxima reach, of groups of threads if those are enough
-    if (hits > K) {
+    if (hits >= K) {
       float q[NT / 64], g;  // the maxima; the largest of each group of NT / 64
       if constexpr (NT == 64) {
         g = q[0] = best;
@@ -197,7 +197,7 @@ __device__ __forceinline__ void select_chunk(Selection<NT>& S, Progress& p, int 
           g = fmaxf(g, q[w]);
         }
       }
-      if (K <= 40 && (int)__popcll(__ballot(g >= from)) >= K) {
+      if (K <= (NT == 64 ? 64 : 40) && (int)__popcll(__ballot(g >= from)) >= K) {
         from = fmaxf(from, kth_of_wave(g, K, S.group[threadIdx.x >> 6]));
       } else {
         const uint32_t k = search(order_key(from), order_key(row_wave_max(g)), K, K + (K >> 3) + 2, [&](uint32_t k) {
@@ -330,10 +330,12 @@ __global__ void __launch_bounds__(NT) k_logprob(LogprobArgs a, int segs, int seg
 #pragma unroll
         for (int e = 0; e < VEC; ++e) best = fmaxf(best, RT::get(v[j], e));
       if (best > st.m) st.lift(best, LOG2E);
+      RowStats<true> part = st.empty();
 #pragma unroll
       for (int j = 0; j < NV; ++j)
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) st.add(RT::get(v[j], e), LOG2E);
+        for (int e = 0; e < VEC; ++e) part.add(RT::get(v[j], e), LOG2E);
+      st.join(part);
       if (a.K > 0) {
         const int base = (int)from + (int)threadIdx.x * VEC;
         select_chunk<NT, NE, false>(S, p, a.K, best, [&](int j, float& x, int& c) {
@@ -431,18 +433,31 @@ __global__ void __launch_bounds__(JOIN_T) k_logprob_join(LogprobArgs a, int segs
 
 constexpr int SEGS = 1024;  // segments of all rows that are split
 
-template <class T, int NT, int NV, bool ONCE = false>
+template <class T, int NT, int NV>
 void whole(const LogprobArgs& a, hipStream_t s) {
   constexpr int64_t GRID = 1 << 20;  // workgroups walk the rows beyond
-  hipLaunchKernelGGL((k_logprob<T, NT, NV, false, ONCE>), dim3((unsigned)std::min<int64_t>(a.R, GRID)), dim3(NT), 0, s, a, 1, a.C);
+  const dim3 grid((unsigned)std::min<int64_t>(a.R, GRID));
+  // more than the last-level cache holds is not kept there: 2048 x 131072 fp32 204 us against 197
+  if (NT <= 256 && beyond_cache((int64_t)a.R * a.C * (int)sizeof(T))) hipLaunchKernelGGL((k_logprob<T, NT, NV, false, NT <= 256>), grid, dim3(NT), 0, s, a, 1, a.C);
+  else hipLaunchKernelGGL((k_logprob<T, NT, NV, false, false>), grid, dim3(NT), 0, s, a, 1, a.C);
 }
 
 template <class T>
 void launch_t(const LogprobArgs& a, hipStream_t s) {
   constexpr int VEC = RowT<T>::VEC, NV = 16 / VEC;  // 16 logits a thread at a time: with 32, registers limit the waves (bf16, 2048 x 131072: 258 us against 179)
-  // a wave per row, as long as its 64 maxima tell the K best from the rest (96 rows of
-  // 1000, fp32, 4.9 us at K = 5; at K = 64 four waves take 7.6 us against 64)
-  if (a.C <= 2048 && a.K <= 40) return whole<T, 64, NV>(a, s);
+  // a wave per row for short or many rows, as long as its 64 maxima tell the K best from the
+  // rest (fp32: 96 rows of 1000, K = 5, 4.8 us against 5.4 with two waves; 60000 of 2049, K = 16,
+  // 151 against 205 and, with four, 338; 8000 of 32768 199 against 209 and 221; 16000 of 1000 at K = 41
+  // 35 against 61, at K = 64 158 against 66), with no more logits a thread than the row has
+  // (300000 rows of 100 218 us with 4, 370 with 16)
+  if (a.K <= 48) {
+    if (a.C <= 64 * VEC) return whole<T, 64, 1>(a, s);
+    if (a.C <= 128 * VEC && NV > 2) return whole<T, 64, 2>(a, s);
+    if (a.C <= 2048 || a.R >= 4000) return whole<T, 64, NV>(a, s);
+  }
+  // two waves for fewer rows or more alternatives (2000 of 10000, K = 20, 28 us against 32 with one
+  // or four; 2000 of 1000, K = 64, 12 against 19 with four; 16000 of 1000 at K = 128 628 against 146)
+  if (a.K <= 80 && (a.C <= 2048 || a.R >= 2000)) return whole<T, 128, NV>(a, s);
   // few long rows in segments, down to the numbers of rows where whole ones take as long
   // (fp32, K = 20: one row of 131072 classes 10.7 us against 29.4, 61 rows 21 against 35, 200
   // rows 38 against 39; of 32000 10.4 against 11.7, 61 rows 12.9 against 13.1, 128 rows 15.1
@@ -462,9 +477,6 @@ void launch_t(const LogprobArgs& a, hipStream_t s) {
   // 79; 512 rows 76, 64 and 82; 1000 rows of 10000 34, 23 and 18)
   if (a.R < 512 && a.C > 8192) return whole<T, 1024, NV>(a, s);
   if ((a.R < 512 && a.C > 4096) || (a.R < 1024 && a.C > 32768)) return whole<T, 512, NV>(a, s);
-  // more than the last-level cache holds is not kept there: 2048 x 131072 fp32 204 us
-  // against 197
-  if (beyond_cache((int64_t)a.R * a.C * sizeof(T))) return whole<T, 256, NV, true>(a, s);
   return whole<T, 256, NV>(a, s);
 }
 

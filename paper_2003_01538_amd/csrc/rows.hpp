@@ -267,6 +267,17 @@ struct RowStats {
     s += e;
     if constexpr (T) t = fmaf(e, fmaxf(d, FAR), t);
   }
+  // A chunk's sums are made apart and joined, so that a long row's roundings are those of
+  // as many additions as it has chunks rather than classes.
+  __device__ __forceinline__ RowStats empty() const {
+    RowStats r;
+    r.m = m;
+    return r;
+  }
+  __device__ __forceinline__ void join(const RowStats& chunk) {
+    s += chunk.s;
+    if constexpr (T) t += chunk.t;
+  }
   template <int NT>
   __device__ __forceinline__ void over_block(float k2, float (*sh)[2]) {
     lift(block_max<NT>(m, &sh[0][0]), k2);

@@ -264,3 +264,32 @@ def test_same_bits_every_time(gpu_lib):
 @pytest.mark.parametrize("R,C", [(99, 17000), (100, 17000), (199, 33000), (200, 33000)])
 def test_row_counts_around_the_split(gpu_lib, R, C, prec):
     Call(logits(R, C, 13), prec, 2, 20).run().check()
+
+
+@pytest.mark.parametrize("prec", [BF, F])
+@pytest.mark.parametrize("C", [1, 37, 100, 255, 256, 257, 511, 512, 513, 600])
+def test_short_rows(gpu_lib, C, prec):
+    for K in (1, 20, 48, 49, 80, 81, 128):
+        Call(logits(33, C, 14), prec, 1, K, pad=C % 3).run().check()
+
+
+@pytest.mark.parametrize("prec", [BF, F])
+@pytest.mark.parametrize("R,C,K", [(1999, 2100, 5), (2000, 2100, 5), (2000, 2100, 80), (2000, 2100, 81), (3999, 2100, 48), (4000, 2100, 48), (4000, 2100, 49)])
+def test_many_rows(gpu_lib, R, C, K, prec):
+    Call(logits(R, C, 15), prec, 1, K).run().check()
+
+
+@pytest.mark.parametrize("prec", [BF, F])
+@pytest.mark.parametrize("K", [1, 37, 70])
+@pytest.mark.parametrize("kind", ["rising", "falling", "equal", "few", "steps", "late"])
+def test_orders_that_are_hard_for_a_wave(gpu_lib, kind, K, prec):
+    # more rows than are given four waves; all alike, so that one is compared and the others with it
+    C, R = 9000, 4000
+    i = torch.arange(C, device="cuda", dtype=torch.float32)
+    z = {"rising": i / C * 40 - 20, "falling": -i / C * 40, "equal": torch.full((C,), 1.5, device="cuda"),
+         "few": torch.where(i % 1000 == 7, 3.0, 0.0), "steps": torch.floor(i / 700), "late": torch.where(i > C - 200, 5.0, 0.0)}[kind]
+    one = Call(z[None], prec, 1, K, classes=torch.tensor([[5]])).run().check()
+    all_ = Call(z[None].expand(R, C), prec, 1, K, classes=torch.full((R, 1), 5)).run()
+    assert bool((all_.ids.view == one.ids.view).all())
+    # another split of the same sums: the two are each within the tolerance of check()
+    near(all_.best.numpy(), np.broadcast_to(one.best.numpy(), (R, K)), lambda v: 2 * (256 + 8 * 20) * U + 16 * U * np.abs(v))
