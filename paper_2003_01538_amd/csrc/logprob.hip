@@ -109,13 +109,13 @@ __device__ __forceinline__ void cut(Selection<NT>& S, Progress& p, int K) {
   __syncthreads();
 }
 
-// The K-th largest of the 64 lanes' values, K <= 64; `sh`: the wave's own 64 floats.
-__device__ __forceinline__ float kth_of_wave(float g, int K, float* sh) {
-  sh[threadIdx.x & 63] = g;
+// The K-th largest of the 64 lanes' values, K <= 64; `own`: the wave's 64 floats, aligned to 16 bytes.
+__device__ __forceinline__ float kth_of_wave(float g, int K, float* own) {
+  own[threadIdx.x & 63] = g;
   int before = 0;
 #pragma unroll
   for (int i = 0; i < 64; i += 4) {
-    const floatx4 q = *reinterpret_cast<const floatx4*>(sh + i);
+    const floatx4 q = *reinterpret_cast<const floatx4*>(own + i);
 #pragma unroll
     for (int e = 0; e < 4; ++e) before += q[e] > g ? 1 : 0;
   }
