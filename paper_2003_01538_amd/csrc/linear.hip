@@ -2,7 +2,7 @@
 // y[m][n] = act(sum_k x[m][k] w[n][k] + bias[n] (+ res)) (+ res).
 //
 // Three kernels.  k_linear_few is for outputs of few tiles: a workgroup makes a
-// small tile and its waves split the reduction, each loading its operands
+// small tile, 16 x 16 to 64 x 32, and its waves split the reduction, each loading its operands
 // straight into registers (nothing is shared, so nothing is staged), and their
 // sums meet in LDS in wave order.  k_linear_stream is its form for up to 64 aligned
 // rows.  k_linear_tile is for many tiles: operands go through LDS, each wave sums
@@ -35,6 +35,7 @@ namespace {
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef u32x4 u32x4_at2 __attribute__((aligned(2)));
+typedef u32x4 u32x4_at4 __attribute__((aligned(4)));
 typedef u32x2 u32x2_at2 __attribute__((aligned(2)));
 typedef floatx4 floatx4_at4 __attribute__((aligned(4)));
 
@@ -64,14 +65,33 @@ template <> struct LinT<float> {
   }
 };
 
-// 16 bytes of a row at any element: the hardware takes vector accesses at every
-// byte address.
-template <class T>
-__device__ __forceinline__ u32x4 full_piece(const T* row, int k) {
-  return *reinterpret_cast<const u32x4_at2*>(row + k);
-}
+// 16 bytes of a row at any element: the hardware takes vector accesses at every byte
+// address, but those between two words (bf16 rows an odd number of elements apart) at down
+// to a third of the rate.  ODD: some rows lie so; the words that hold the 16 bytes are
+// loaded, and shifted when they have arrived.  (The halves of words beside the 16 bytes
+// go nowhere; no word is loaded that holds nothing of the row.)  In k_linear_tile, whose
+// loads have a K-tile's time, this gained nothing (4096^3 227 us against 214).
+template <bool ODD> struct Piece {
+  u32x4 v;
+  template <class T> __device__ __forceinline__ void load(const T* at) { v = *reinterpret_cast<const u32x4_at4*>(at); }
+  __device__ __forceinline__ u32x4 get() const { return v; }
+};
+template <> struct Piece<true> {
+  u32x4 v;
+  uint32_t last, shift;
+  template <class T> __device__ __forceinline__ void load(const T* at) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(at), odd = a & 2;
+    v = *reinterpret_cast<const u32x4_at4*>(a - odd);
+    last = *reinterpret_cast<const uint32_t*>(a - odd + 12 + 2 * odd);  // the fourth word again, or the one behind it
+    shift = uint32_t(odd) * 8;
+  }
+  __device__ __forceinline__ u32x4 get() const {
+    return u32x4{__builtin_amdgcn_alignbit(v[1], v[0], shift), __builtin_amdgcn_alignbit(v[2], v[1], shift),
+                 __builtin_amdgcn_alignbit(v[3], v[2], shift), __builtin_amdgcn_alignbit(last, v[3], shift)};
+  }
+};
 
-// The same with zeros behind the row's end: the last 16 bytes of the row, shifted.
+// 16 bytes with zeros behind the row's end: the last 16 bytes of the row, shifted.
 template <class T>
 __device__ __forceinline__ u32x4 piece(const T* row, int k, int K) {
   constexpr int VEC = LinT<T>::VEC;
@@ -82,7 +102,7 @@ __device__ __forceinline__ u32x4 piece(const T* row, int k, int K) {
     return __builtin_bit_cast(u32x4, t);
   }
   const int from = min(k, K - VEC), bits = min(k - from, VEC) * (int)sizeof(T) * 8;
-  const u32x4 v = full_piece(row, from);
+  const u32x4 v = *reinterpret_cast<const u32x4_at2*>(row + from);
   const uint64_t lo = v[0] | uint64_t(v[1]) << 32, hi = v[2] | uint64_t(v[3]) << 32;
   uint64_t l = lo, h = hi;
   if (bits >= 128) {
@@ -205,7 +225,7 @@ __device__ __forceinline__ void finish4(const LinearArgs& a, int m, int n, float
 // 128 bytes of each row: lane group g = lane / 16 takes 32 of them in two
 // pieces, so that a step's loads use whole cache lines.  Wave w takes steps w,
 // w + NW, ..., U of them in flight.
-template <class T, int FM, int FN, int NW, int U>
+template <class T, int FM, int FN, int NW, int U, bool ODD>
 __global__ void __launch_bounds__(NW * 64) k_linear_few(LinearArgs a) {
   using L = LinT<T>;
   constexpr int VEC = L::VEC, STEP = 8 * VEC;
@@ -241,41 +261,51 @@ __global__ void __launch_bounds__(NW * 64) k_linear_few(LinearArgs a) {
 #pragma unroll
     for (int j = 0; j < FN; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
 
-  u32x4 w[U][FN][2], x[U][FM][2];
-  auto products = [&](int u) {
+  auto products = [&](const u32x4 (&w)[FN][2], const u32x4 (&x)[FM][2]) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int i = 0; i < FM; ++i)
 #pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = L::mma16(w[u][j][h], x[u][i][h], acc[i][j]);
+        for (int j = 0; j < FN; ++j) acc[i][j] = L::mma16(w[j][h], x[i][h], acc[i][j]);
   };
+  u32x4 w[FN][2], x[FM][2];
   int k = wave * STEP;
   for (; k + (U - 1) * NW * STEP + STEP <= a.K; k += U * NW * STEP) {
+    Piece<ODD> pw[U][FN][2], px[U][FM][2];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int ku = k + u * NW * STEP + off;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
 #pragma unroll
-        for (int j = 0; j < FN; ++j) w[u][j][h] = full_piece(wr[j], ku + h * VEC);
+        for (int j = 0; j < FN; ++j) pw[u][j][h].load(wr[j] + ku + h * VEC);
 #pragma unroll
-        for (int i = 0; i < FM; ++i) x[u][i][h] = full_piece(xr[i], ku + h * VEC);
+        for (int i = 0; i < FM; ++i) px[u][i][h].load(xr[i] + ku + h * VEC);
       }
     }
     __builtin_amdgcn_sched_barrier(0);  // all loads are under way before the first product waits
 #pragma unroll
-    for (int u = 0; u < U; ++u) products(u);
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j) w[j][h] = pw[u][j][h].get();
+#pragma unroll
+        for (int i = 0; i < FM; ++i) x[i][h] = px[u][i][h].get();
+      }
+      products(w, x);
+    }
   }
   for (; k < a.K; k += NW * STEP) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
 #pragma unroll
-      for (int j = 0; j < FN; ++j) w[0][j][h] = piece(wr[j], k + off + h * VEC, a.K);
+      for (int j = 0; j < FN; ++j) w[j][h] = piece(wr[j], k + off + h * VEC, a.K);
 #pragma unroll
-      for (int i = 0; i < FM; ++i) x[0][i][h] = piece(xr[i], k + off + h * VEC, a.K);
+      for (int i = 0; i < FM; ++i) x[i][h] = piece(xr[i], k + off + h * VEC, a.K);
     }
-    products(0);
+    products(w, x);
   }
 
 #pragma unroll
@@ -426,7 +456,7 @@ __global__ void __launch_bounds__(WM * WN * 64) k_linear_tile(LinearArgs a) {
     auto row = [&](int p) { return reinterpret_cast<const T*>(reinterpret_cast<const char*>(p < PA ? xb : wb) + off[p]); };
     if (k0 + KT <= a.K) {  // the same for the whole workgroup
 #pragma unroll
-      for (int p = 0; p < PA + PB; ++p) reg[p] = full_piece(row(p), k0 + kc);
+      for (int p = 0; p < PA + PB; ++p) reg[p] = *reinterpret_cast<const u32x4_at2*>(row(p) + k0 + kc);
     } else {
 #pragma unroll
       for (int p = 0; p < PA + PB; ++p) reg[p] = piece(row(p), k0 + kc, a.K);
@@ -642,10 +672,17 @@ __global__ void __launch_bounds__(WM * WN * 64) k_linear_tile(LinearArgs a) {
   }
 }
 
+// Whether rows of bf16 lie between two words.
+template <class T>
+bool odd_rows(const LinearArgs& a) {
+  return sizeof(T) == 2 && (((a.ldx | a.ldw) & 1) || ((reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.w)) & 2));
+}
+
 template <class T, int FM, int FN, int NW, int U>
 void few(const LinearArgs& a, hipStream_t s) {
-  const int64_t tiles = (int64_t)((a.N + 16 * FN - 1) / (16 * FN)) * ((a.M + 16 * FM - 1) / (16 * FM));
-  hipLaunchKernelGGL((k_linear_few<T, FM, FN, NW, U>), dim3((unsigned)tiles), dim3(NW * 64), 0, s, a);
+  const dim3 tiles((unsigned)(((a.N + 16 * FN - 1) / (16 * FN)) * ((int64_t)(a.M + 16 * FM - 1) / (16 * FM))));
+  if (sizeof(T) == 2 && odd_rows<T>(a)) hipLaunchKernelGGL((k_linear_few<T, FM, FN, NW, U, sizeof(T) == 2>), tiles, dim3(NW * 64), 0, s, a);
+  else hipLaunchKernelGGL((k_linear_few<T, FM, FN, NW, U, false>), tiles, dim3(NW * 64), 0, s, a);
 }
 
 template <class T, int FM, int NW, int S>
@@ -663,39 +700,43 @@ void tile(const LinearArgs& a, hipStream_t s) {
 // one workgroup of each, in us: one / `fit` of them on a CU, measured at 128 to 4096
 // rows, 4096 features and K = 4096, and what a round of workgroups costs besides.
 // One row per kernel, by type and by how the loads go.
-enum Kernel { FEW_32x32, FEW_64x32, TILE_64x64, TILE_64x128, TILE_128x128, TILE_256x128, TILE_256x256, KERNELS };
+enum Kernel { FEW_16x16, FEW_32x16, FEW_32x32, FEW_64x32, TILE_64x64, TILE_64x128, TILE_128x128, TILE_256x128, TILE_256x256, KERNELS };
 struct Cost {
   int bm, bn, fit;
   float alone, full, round;
 };
 // Where a kernel is not built, its cost is 0.
-constexpr Cost COSTS[2][2][KERNELS] = {
-    {   // bf16, loads through registers
-     {{32, 32, 2, .60f, 1.18f, 2.5f}, {64, 32, 2, .88f, 1.75f, 2.5f}, {64, 64, 4, 1.02f, 1.65f, 3.f}, {}, {128, 128, 2, 1.72f, 1.74f, 6.f}, {}, {256, 256, 1, 3.1f, 3.1f, 16.f}},
-        // bf16, loads into LDS
-     {{32, 32, 2, .245f, .456f, 2.5f}, {64, 32, 2, .345f, .67f, 2.5f}, {64, 64, 2, .33f, .50f, 3.f}, {64, 128, 2, .44f, .74f, 4.f}, {128, 128, 2, .62f, 1.03f, 7.f}, {256, 128, 1, .94f, .94f, 9.f}, {256, 256, 1, 1.48f, 1.48f, 16.f}}},
-    {   // fp32, loads through registers
-     {{32, 32, 2, .28f, .53f, 2.5f}, {64, 32, 2, .50f, .99f, 2.5f}, {64, 64, 2, 1.28f, 1.5f, 3.f}, {}, {128, 128, 2, 3.1f, 4.35f, 6.f}, {}, {256, 256, 1, 8.2f, 8.2f, 16.f}},
-        // fp32, loads into LDS: the matrix cores' rate, 7.4 us for 256 x 256 outputs
-     {{32, 32, 2, .277f, .53f, 2.5f}, {64, 32, 2, .50f, .97f, 2.5f}, {64, 64, 2, 1.15f, 1.22f, 3.f}, {64, 128, 2, 1.13f, 2.26f, 4.f}, {128, 128, 2, 2.06f, 3.95f, 6.f}, {256, 128, 1, 3.85f, 3.85f, 9.f}, {256, 256, 1, 7.45f, 7.45f, 16.f}}},
+enum Loads { BF16_ODD, BF16_REGISTERS, BF16_LDS, F32_REGISTERS, F32_LDS };
+constexpr Cost COSTS[5][KERNELS] = {
+    // bf16, loads through registers, some rows between two words
+    {{16, 16, 2, .242f, .419f, 3.5f}, {32, 16, 2, .352f, .603f, 3.5f}, {32, 32, 2, .45f, .77f, 2.5f}, {64, 32, 2, .60f, 1.07f, 2.5f}, {64, 64, 4, 1.02f, 1.65f, 3.f}, {}, {128, 128, 2, 1.72f, 1.74f, 6.f}, {}, {256, 256, 1, 3.1f, 3.1f, 16.f}},
+    // bf16, loads through registers
+    {{16, 16, 2, .145f, .255f, 3.5f}, {32, 16, 2, .219f, .395f, 3.5f}, {32, 32, 2, .303f, .517f, 2.5f}, {64, 32, 2, .41f, .766f, 2.5f}, {64, 64, 4, .89f, 1.33f, 3.f}, {}, {128, 128, 2, 1.58f, 1.66f, 6.f}, {}, {256, 256, 1, 2.8f, 2.8f, 16.f}},
+    // bf16, loads into LDS
+    {{16, 16, 2, .103f, .205f, 3.5f}, {32, 16, 2, .157f, .328f, 3.5f}, {32, 32, 2, .245f, .456f, 2.5f}, {64, 32, 2, .345f, .67f, 2.5f}, {64, 64, 2, .33f, .50f, 3.f}, {64, 128, 2, .44f, .74f, 4.f}, {128, 128, 2, .62f, 1.03f, 7.f}, {256, 128, 1, .94f, .94f, 9.f}, {256, 256, 1, 1.48f, 1.48f, 16.f}},
+    // fp32, loads through registers
+    {{16, 16, 2, .105f, .22f, 3.5f}, {32, 16, 2, .16f, .34f, 3.5f}, {32, 32, 2, .28f, .53f, 2.5f}, {64, 32, 2, .50f, .99f, 2.5f}, {64, 64, 2, 1.28f, 1.5f, 3.f}, {}, {128, 128, 2, 3.1f, 4.35f, 6.f}, {}, {256, 256, 1, 8.2f, 8.2f, 16.f}},
+    // fp32, loads into LDS: the matrix cores' rate, 7.4 us for 256 x 256 outputs
+    {{16, 16, 2, .105f, .22f, 3.5f}, {32, 16, 2, .16f, .34f, 3.5f}, {32, 32, 2, .277f, .53f, 2.5f}, {64, 32, 2, .50f, .97f, 2.5f}, {64, 64, 2, 1.15f, 1.22f, 3.f}, {64, 128, 2, 1.13f, 2.26f, 4.f}, {128, 128, 2, 2.06f, 3.95f, 6.f}, {256, 128, 1, 3.85f, 3.85f, 9.f}, {256, 256, 1, 7.45f, 7.45f, 16.f}},
 };
 
 // The kernel with the least time by those costs: whole rounds of the chip and the
 // rest.  (bf16, K = 4096: 512 x 4096 outputs 64 x 128 32 us against 36 for 64 x 64 and
 // 44 for 128 x 128; 1024 x 4096 128 x 128 45 against 66 and, 256 x 256, 86; 2048 x 4096
-// 256 x 128 69 against 75 and 91; 4096 x 4096 256 x 256 114 against 134 for 256 x 128.)
-Kernel pick(const LinearArgs& a, bool f32, bool dma, bool near, double* us) {
-  const int64_t steps = ((int64_t)a.K * (f32 ? 4 : 2) + ROW - 1) / ROW;
-  Kernel best = FEW_32x32;
+// 256 x 128 69 against 75 and 91; 4096 x 4096 256 x 256 114 against 134 for 256 x 128; 41 x
+// 58, K = 18939, 16 x 16 89 before and 54 after shifting odd rows, 32 x 32 177.)
+Kernel pick(const LinearArgs& a, Loads loads, bool near, double* us) {
+  const int64_t steps = ((int64_t)a.K * (loads < F32_REGISTERS ? 2 : 4) + ROW - 1) / ROW;
+  Kernel best = FEW_16x16;
   double least = 0;
   for (int k = 0; k < (near ? KERNELS : TILE_64x64); ++k) {
-    const Cost& c = COSTS[f32][dma][k];
+    const Cost& c = COSTS[loads][k];
     if (!c.bm) continue;
     const int64_t n = ((a.M + c.bm - 1) / c.bm) * (int64_t)((a.N + c.bn - 1) / c.bn), round = 256 * c.fit;
     const int64_t whole = n / round, rest = n % round;
-    // more than one on some CUs: the slowest CU's time, or, for the kernels bound by L2, a share of all
+    // more than one on some CUs: the slowest CU's time, or, for the two kernels bound by L2, a share of all
     double last = rest <= 256 ? c.alone : c.full;
-    if (k < TILE_64x64 && rest > 256) last = c.alone + (c.full - c.alone) * (double)(rest - 256) / (double)(round - 256);
+    if ((k == FEW_32x32 || k == FEW_64x32) && rest > 256) last = c.alone + (c.full - c.alone) * (double)(rest - 256) / (double)(round - 256);
     const double t = whole * (steps * (double)c.full + c.round) + (rest ? steps * last + c.round : 0);
     if (k == 0 || t < least) {
       least = t;
@@ -707,12 +748,15 @@ Kernel pick(const LinearArgs& a, bool f32, bool dma, bool near, double* us) {
 }
 
 // What k_linear_stream takes for blocks of 16 rows, in us: a workgroup brings 47 GB/s
-// from L2 (12 TB/s in all), the chip 5.5 TB/s of weights from memory.  (4096 features, K
-// = 4096, bf16: 16 rows 9.1 us, k_linear_few 10.1; 32 rows 10.9 and 14.3; 48 rows 12.7
-// and 17.5; 64 rows 14.3 and 18.3.  K = 25088: 32 rows 51 and 72, 64 rows 71 and 93.)
+// from L2 (12 TB/s in all), up to 95 of bf16 where there are fewer of them, the chip 5.5
+// TB/s of weights from memory.  (4096 features, K = 4096, bf16: 16 rows 9.1 us,
+// k_linear_few 10.1; 32 rows 10.9 and 14.3; 48 rows 12.7 and 17.5; 64 rows 14.3 and 18.3.
+// K = 25088: 32 rows 51 and 72, 64 rows 71 and 93.  48 x 64, K = 11136: 17 and 22; 54 x 832
+// fp32, K = 5760, 42 and 20.)
 double stream_us(const LinearArgs& a, int blocks, int es) {
-  const double step = (double)a.K * es;
-  return 2. + std::max(((a.N + 15) / 16 + 255) / 256 * (16. + 16. * blocks) * step / 47e3, a.N * step / 5.5e6);
+  const double row = (double)a.K * es;
+  const int groups = (a.N + 15) / 16, rounds = (groups + 255) / 256;
+  return 2. + std::max(rounds * (16. + 16. * blocks) * row / (es == 2 ? std::min(95e3, 12e6 / std::min(groups, 256)) : 47e3), a.N * row / 5.5e6);
 }
 
 template <class T>
@@ -726,9 +770,10 @@ void launch_t(const LinearArgs& a, hipStream_t s) {
   const bool near = (255 * std::max(a.ldx, a.ldw) + a.K) * (int64_t)sizeof(T) < (int64_t(1) << 31);
   // up to 8 rows the weights are all there is to read: 16 features a workgroup (4096
   // features, K = 25088, bf16: 37 us for one row, 5.5 TB/s; with 8 waves 42)
-  if (a.M <= 8 || (a.M <= 16 && !(dma && near))) return few<T, 1, 1, 16, 2>(a, s);
+  if (a.M <= 8) return few<T, 1, 1, 16, 2>(a, s);
+  const Loads loads = F ? (dma ? F32_LDS : F32_REGISTERS) : dma ? BF16_LDS : odd_rows<T>(a) ? BF16_ODD : BF16_REGISTERS;
   double us;
-  const Kernel k = pick(a, F, dma, near, &us);
+  const Kernel k = pick(a, loads, near, &us);
   if (a.M <= 64 && dma && near) {
     const int blocks = (a.M + 15) / 16;
     if (stream_us(a, blocks, sizeof(T)) < us) {
@@ -737,10 +782,10 @@ void launch_t(const LinearArgs& a, hipStream_t s) {
       if (blocks == 3) return stream<T, 3, 6, 3>(a, s);
       return stream<T, 4, 4, 3>(a, s);
     }
-  } else if (a.M <= 32) {
-    return few<T, 2, 1, 16, 2>(a, s);
   }
   switch (k) {
+    case FEW_16x16: return few<T, 1, 1, 16, 2>(a, s);
+    case FEW_32x16: return few<T, 2, 1, 16, 2>(a, s);
     case FEW_32x32: return few<T, 2, 2, 8, 2>(a, s);
     case FEW_64x32: return few<T, 4, 2, 8, 1>(a, s);
     case TILE_64x64: return dma ? tile<T, 64, 64, 1, 2, true, 4>(a, s) : tile<T, 64, 64, 2, 2, false, 2>(a, s);

@@ -264,3 +264,16 @@ def test_more_outputs_than_a_launch_has_threads(gpu_lib, M, N):
         want = x.view[rows].float() * w.view.float().t() + b
         assert torch.equal(y.view[rows], (want if r is None else want + r.view.float()).bfloat16()), m
     assert bool((y.buf[-64:] == MARK).all())
+
+
+@pytest.mark.parametrize("prec", [BF, F])
+@pytest.mark.parametrize("pad,lead", [(0, 0), (1, 0), (0, 1), (3, 2), (2, 1), (8, 0)])
+@pytest.mark.parametrize("M,N,K", [(9, 20, 900), (41, 58, 2049), (70, 130, 4100), (120, 339, 1001), (300, 300, 263), (12, 40, 9)])
+def test_rows_between_two_words_in_small_tiles(gpu_lib, M, N, K, pad, lead, prec):
+    x, w, b, r, y = make(M, N, K, prec, prec, True, pads=(pad, pad, 0, 0), leads=(lead, lead, 0, 0), seed=13)
+    for t in (x, w):  # what lies beside the rows is read into no sum
+        keep = t.view.clone()
+        t.buf.fill_(float("nan"))
+        t.view.copy_(keep)
+    call(x, w, b, r, y, prec, prec, 0, 0)
+    check(x, w, b, r, y, prec, 0, 0)
