@@ -380,7 +380,7 @@ Cut cut_row(int C, int chunk, int64_t want) {
   const int chunks = (int)(((int64_t)C + chunk - 1) / chunk);
   const int n = (int)std::max<int64_t>(1, std::min<int64_t>(chunks, want));
   const int per = (chunks + n - 1) / n;
-  return {(chunks + per - 1) / per, per * chunk};
+  return {(chunks + per - 1) / per, (int)std::min<int64_t>((int64_t)per * chunk, INT32_MAX)};
 }
 
 template <class T, int NT, bool PARTS, bool ONCE>

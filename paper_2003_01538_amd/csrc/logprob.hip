@@ -21,7 +21,7 @@
 // segments' statistics and K best go to the scratch memory, and a second launch
 // joins them with the same selection.
 //
-// What bounds it: memory for many rows (2048 x 131072 fp32, K = 20, 200 us, 5.4 TB/s);
+// What bounds it: memory for many rows (2048 x 131072 fp32, K = 20, 188 us, 5.7 TB/s);
 // for few the chain of loads, reductions and selection of a workgroup, two of them when
 // rows are split (one row of 131072 6.2 + 5.1 us).
 #include "rows.hpp"

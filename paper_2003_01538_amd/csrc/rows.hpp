@@ -54,8 +54,9 @@ template <> struct RowT<uint16_t> {  // bf16
   }
 };
 
-// Whether a call that moves so many bytes gains by keeping none of them in a cache:
-// twice the last-level cache and more.
+// Whether a call that moves so many bytes gains by keeping none of them in a cache: well
+// beyond the last-level one of 256 MB (distillation with gradients, fp32, 4096 rows of 16384, 537 MB,
+// 105 us against 111; 2048 rows, 268 MB, the same tensors again and again, 47 against 46).
 inline bool beyond_cache(int64_t bytes) { return bytes > int64_t(400) << 20; }
 
 // A vector of a row.  ONCE: no cache is to keep it.

@@ -271,3 +271,31 @@ def test_same_bits_every_time(gpu_lib):
         c.run()
         seen.append((c.loss.view.clone(), c.stats.view.clone(), c.grad.view.clone()))
     assert all(torch.equal(a, b) for s in seen[1:] for a, b in zip(s, seen[0]))
+
+
+@pytest.mark.parametrize("prec,R,C", [(BF, 3300, 32769), (BF, 8300, 16384), (F, 13000, 4101), (F, 800, 70001), (BF, 30000, 4500)])
+def test_more_than_the_caches_hold(gpu_lib, prec, R, C):
+    # such calls go past the caches; the same rows, fewer at a time, do not: equal to the last bit
+    K, es = 7, 2 if prec == BF else 4
+    assert 2 * R * C * es > 400 << 20
+    g = torch.Generator(device="cuda").manual_seed(R)
+    z = Rows(R, C, dtype_of(prec), 0, 0, torch.randn(R, C, device="cuda", generator=g) * 3)
+    ids = torch.randint(0, C, (R, K), device="cuda", generator=g, dtype=torch.int32)
+    u = torch.randn(R, K, device="cuda", generator=g)
+    weight = torch.rand(R, device="cuda", generator=g)
+
+    def run(first, n):
+        loss, stats = torch.empty(n, device="cuda"), torch.empty(n, 2, device="cuda")
+        one, two = Rows(n, C, dtype_of(prec)), Rows(n, C, dtype_of(prec))
+        head = (z.ptr + first * C * es, C, n, C, prec, ids[first:].data_ptr(), u[first:].data_ptr(), K, 2.0, weight[first:].data_ptr())
+        fsb.fs_distill_device(*head, loss.data_ptr(), stats.data_ptr(), one.ptr, C, 0, stream())
+        fsb.fs_distill_grad_device(*head, stats.data_ptr(), two.ptr, C, stream())
+        assert one.untouched() and two.untouched()
+        return loss, stats, one.view, two.view
+
+    whole = run(0, R)
+    for first in range(0, R, -(-R // 4)):
+        n = min(R - first, -(-R // 4))
+        for a, b in zip(whole, run(first, n)):
+            assert torch.equal(a[first:first + n], b), first
+    assert z.untouched()

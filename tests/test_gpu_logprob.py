@@ -293,3 +293,18 @@ def test_orders_that_are_hard_for_a_wave(gpu_lib, kind, K, prec):
     assert bool((all_.ids.view == one.ids.view).all())
     # another split of the same sums: the two are each within the tolerance of check()
     near(all_.best.numpy(), np.broadcast_to(one.best.numpy(), (R, K)), lambda v: 2 * (256 + 8 * 20) * U + 16 * U * np.abs(v))
+
+
+@pytest.mark.parametrize("prec,R,C,K", [(F, 4100, 26000, 9), (BF, 2100, 101000, 20), (F, 1100, 100001, 30), (F, 4400, 24001, 100)])
+def test_more_than_the_caches_hold(gpu_lib, prec, R, C, K):
+    # such calls go past the caches; a few of their rows against the definition, the others' alternatives by sorting
+    z = logits(R, C, 16)
+    assert R * C * (2 if prec == BF else 4) > 400 << 20
+    c = Call(z, prec, 1, K).run()
+    for r in (0, R // 2, R - 1):
+        want = ref.logprob(c.z.numpy()[r:r + 1], c.classes[r:r + 1].cpu().numpy(), K)
+        assert np.array_equal(c.ids.numpy()[r:r + 1], want["top_ids"])
+        near(c.logp.numpy()[r:r + 1], want["logp"], lambda v: (128 + 8 * np.abs(v)) * U)
+        near(c.entropy.numpy()[r:r + 1, 0], want["entropy"], lambda v: (128 + 48 * (1 + math.log(C))) * U)
+    top = c.z.view.float().sort(dim=1, descending=True, stable=True)
+    assert torch.equal(c.ids.view, top.indices[:, :K].int())
