@@ -448,8 +448,9 @@ fs_status fs_conv_bf16_device_noalloc(const void *d_in, int32_t B, int32_t H, in
  *  - errors leave a message with fs_last_error(NULL). */
 
 /* What is applied to a product: v, max(0, v), v * Phi(v) (Phi: the normal
- * distribution function), v / (1 + e^-v).  A NaN stays NaN, except that RELU
- * gives 0 for it, as it does everywhere in the library. */
+ * distribution function), v / (1 + e^-v).  Their own error is relative, for fp32
+ * outputs at most 16 steps of 2^-24 wherever the exponential is a normal number.
+ * A NaN stays NaN, except that RELU gives 0 for it, as it does everywhere in the library. */
 typedef enum { FS_ACT_NONE = 0, FS_ACT_RELU = 1, FS_ACT_GELU = 2, FS_ACT_SILU = 3 } fs_activation;
 
 /* Matrix product with bias, activation and residual:

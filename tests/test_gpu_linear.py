@@ -277,3 +277,25 @@ def test_rows_between_two_words_in_small_tiles(gpu_lib, M, N, K, pad, lead, prec
         t.view.copy_(keep)
     call(x, w, b, r, y, prec, prec, 0, 0)
     check(x, w, b, r, y, prec, 0, 0)
+
+
+@pytest.mark.parametrize("act", [2, 3])
+@pytest.mark.parametrize("out", [BF, F])
+@pytest.mark.parametrize("M", [1, 300])
+def test_the_tails_of_the_activations(gpu_lib, M, out, act):
+    # s alone through the bias (K = 0), so that nothing but the activation rounds.  GELU for fp32: the
+    # fit 2 steps of U, the reciprocal and its argument 3, the polynomial 4, the exponential with
+    # its correction 3, three products 3; SiLU fewer: 16 for both.  For bf16 the exponent's own roundings
+    # stay, three steps of it; half a step of the value comes last.  Exponentials below 2^-126 may be 0.
+    from scipy.special import log_ndtr
+    v = torch.cat([torch.arange(-13.0, 13.0, 1 / 64), torch.arange(-100.0, 100.0, 0.37)]).cuda()
+    N = len(v)
+    y = Rows(M, N, dtype_of(out))
+    fsb.fs_linear_device(0, 0, 0, 0, v.data_ptr(), 0, 0, y.ptr, y.ld, M, N, 0, BF, out, act, 0, stream())
+    s = v.cpu().numpy().astype(np.float64)
+    with np.errstate(over="ignore"):
+        want = s * np.exp(log_ndtr(s)) if act == 2 else s / (1 + np.exp(-s))
+    exponent = np.minimum(np.abs(s), 13.2) ** 2 / 2 if act == 2 else np.minimum(np.abs(s), 88)
+    steps = 16 * U if out == F else 16 * U + 3 * U * exponent + 2.0 ** -8
+    off = np.abs(y.numpy().astype(np.float64) - want) - (steps * np.abs(want) + np.abs(s) * 2.0 ** -126)
+    assert (off <= 0).all(), (off.max(), s[off.max(0).argmax()])
