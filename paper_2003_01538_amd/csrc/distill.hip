@@ -153,11 +153,12 @@ __device__ __forceinline__ void put_teacher(const DistillArgs& a, T* g, const Te
   }
 }
 
-// The workgroup's stores have been made, those past the caches too: others to the same
-// places come after.  (A wave's own keep their order without.)
-template <int NT>
+// The workgroup's stores have been made: others to the same places come after.  A wave's own
+// ordinary stores keep their order without a wait; that those past the caches (ONCE) keep it
+// with ordinary ones behind them is promised nowhere.
+template <int NT, bool ONCE>
 __device__ __forceinline__ void written() {
-  if constexpr (NT > 64) __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  if constexpr (NT > 64 || ONCE) __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
   __syncthreads();
 }
 
@@ -205,7 +206,7 @@ __global__ void __launch_bounds__(NT, NV > 16 ? 2 : 4) k_distill_held(DistillArg
       t.settle();
       __syncthreads();  // the row and its teacher's classes have been read (the gradient may lie over them)
       put_chunk<T, NT, NV, ONCE>(g, 0, row_end(C), v, gr);
-      written<NT>();
+      written<NT, ONCE>();
       if (us != 0.f) put_teacher<T, NT>(a, g, t, S, st, gr, c, 0, a.C);
     }
     __syncthreads();
@@ -283,7 +284,7 @@ __global__ void __launch_bounds__(NT) k_distill_long(DistillArgs a) {
       t.settle();
       __syncthreads();
       walk_grad<T, NT, NV, false>(z, g, 0, row_end(a.C), gr);
-      written<NT>();
+      written<NT, false>();
       if (us != 0.f) put_teacher<T, NT>(a, g, t, S, st, gr, c, 0, a.C);
     }
     __syncthreads();
@@ -361,7 +362,7 @@ __global__ void __launch_bounds__(NT) k_distill_segment(DistillArgs a, int segs,
       t.settle();
       __syncthreads();  // this segment's classes of the teacher have been read
       walk_grad<T, NT, NV, ONCE>(z, g, first, end, gr);
-      written<NT>();
+      written<NT, ONCE>();
       if (us != 0.f) put_teacher<T, NT>(a, g, t, S, st, gr, c, first, end);
     }
     __syncthreads();

@@ -299,3 +299,43 @@ def test_more_than_the_caches_hold(gpu_lib, prec, R, C):
         for a, b in zip(whole, run(first, n)):
             assert torch.equal(a[first:first + n], b), first
     assert z.untouched()
+
+
+def past_the_caches(R, C, K, prec, step):
+    """Loss, statistics and both gradients of all rows and of a quarter at a time, equal to the last bit,
+    and a few rows against the definition."""
+    es = 2 if prec == BF else 4
+    assert 2 * R * C * es > 400 << 20 >= 2 * -(-R // 4) * C * es
+    g = torch.Generator(device="cuda").manual_seed(R + C)
+    z = (torch.randn(R, C, device="cuda", generator=g) * 3).to(dtype_of(prec))
+    ids = torch.randint(0, C, (R, K), device="cuda", generator=g, dtype=torch.int32)
+    u = torch.randn(R, K, device="cuda", generator=g)
+    weight = torch.rand(R, device="cuda", generator=g)
+
+    def run(first, n):
+        loss, stats = torch.empty(n, device="cuda"), torch.empty(n, 2, device="cuda")
+        one, two = (torch.empty(n, C, dtype=z.dtype, device="cuda") for _ in range(2))
+        head = (z[first:].data_ptr(), C, n, C, prec, ids[first:].data_ptr(), u[first:].data_ptr(), K, 2.0, weight[first:].data_ptr())
+        fsb.fs_distill_device(*head, loss.data_ptr(), stats.data_ptr(), one.data_ptr() if step else 0, C, 0, stream())
+        fsb.fs_distill_grad_device(*head, stats.data_ptr(), two.data_ptr(), C, stream())
+        return (loss, stats, two) + ((one,) if step else ())
+
+    whole = run(0, R)
+    for first in range(0, R, -(-R // 4)):
+        n = min(R - first, -(-R // 4))
+        for a, b in zip(whole, run(first, n)):
+            assert torch.equal(a[first:first + n], b), first
+    for r in (0, R // 2, R - 1):
+        c = Call(z[r:r + 1], ids[r:r + 1], u[r:r + 1], prec, 2.0)
+        c.weight = weight[r:r + 1].contiguous()
+        c.loss.view.copy_(whole[0][r])
+        c.stats.view.copy_(whole[1][r])
+        c.check_loss()
+        for grad in whole[2:]:
+            c.grad.view.copy_(grad[r])
+            c.check_grad()
+
+
+@pytest.mark.parametrize("prec,R,C,K", [(F, 40000, 1500, 128), (F, 52000, 1025, 5), (F, 26000, 2048, 128), (BF, 40000, 3001, 128), (BF, 26000, 4096, 64)])
+def test_one_waves_gradient_past_the_caches(gpu_lib, prec, R, C, K):
+    past_the_caches(R, C, K, prec, False)
