@@ -557,9 +557,17 @@ def fs_bench_conv(B, H, W, Cin, Cout, k, stride, pad, relu=1, residual=0, precis
 
 # Operators on a caller's device tensors.  Every pointer is an integer device
 # address (e.g. torch data_ptr()), 0 for an optional tensor that is not there.
+def _fits(sizes, distances):
+    """Refuses what ctypes would cut to 32 and 64 bits without a word.  Both are
+    the bitwise or of a call's numbers."""
+    if sizes >> 31 not in (0, -1) or distances >> 63 not in (0, -1):
+        raise FsError(FS_ERR_INVALID, "a size does not fit 32 bits, or a row distance 64")
+
+
 def fs_linear_device(d_x, ldx, d_w, ldw, d_bias, d_res, ldres, d_y, ldy, M, N, K, precision, out_precision,
                      activation=FS_ACT_NONE, res_first=0, stream=0):
     """y = act(x . w^T + bias) + res, or act(x . w^T + bias + res)."""
+    _fits(M | N | K, ldx | ldw | ldres | ldy)
     _check(load().fs_linear_device(d_x, ldx, d_w, ldw, d_bias or None, d_res or None, ldres, d_y, ldy, M, N, K,
                                    precision, out_precision, activation, res_first, stream or None))
 
@@ -567,6 +575,7 @@ def fs_linear_device(d_x, ldx, d_w, ldw, d_bias, d_res, ldres, d_y, ldy, M, N, K
 def fs_logprob_device(d_logits, ld, R, C, precision, d_classes, T, K, d_logp, d_entropy, d_top_ids, d_top_logp,
                       d_scratch=0, stream=0):
     """ln p of given classes, entropy and the K most probable classes of each row of logits."""
+    _fits(R | C | T | K, ld)
     _check(load().fs_logprob_device(d_logits, ld, R, C, precision, d_classes or None, T, K, d_logp or None,
                                     d_entropy or None, d_top_ids or None, d_top_logp or None, d_scratch or None,
                                     stream or None))
@@ -575,6 +584,7 @@ def fs_logprob_device(d_logits, ld, R, C, precision, d_classes, T, K, d_logp, d_
 def fs_distill_device(d_logits, ld, R, C, precision, d_top_ids, d_top_logp, K, temperature, d_weight, d_loss, d_stats,
                       d_grad, ldg, d_scratch=0, stream=0):
     """Divergence of each row's softmax from a teacher's top classes, and its gradient."""
+    _fits(R | C | K, ld | ldg)
     _check(load().fs_distill_device(d_logits, ld, R, C, precision, d_top_ids, d_top_logp, K, temperature,
                                     d_weight or None, d_loss or None, d_stats or None, d_grad or None, ldg,
                                     d_scratch or None, stream or None))
@@ -583,6 +593,7 @@ def fs_distill_device(d_logits, ld, R, C, precision, d_top_ids, d_top_logp, K, t
 def fs_distill_grad_device(d_logits, ld, R, C, precision, d_top_ids, d_top_logp, K, temperature, d_weight, d_stats,
                            d_grad, ldg, stream=0):
     """The gradient alone, from fs_distill_device's statistics."""
+    _fits(R | C | K, ld | ldg)
     _check(load().fs_distill_grad_device(d_logits, ld, R, C, precision, d_top_ids, d_top_logp, K, temperature,
                                          d_weight or None, d_stats, d_grad, ldg, stream or None))
 

@@ -74,6 +74,23 @@ def test_distill_wants_an_output():
     assert status(fsb.fs_distill_grad_device, GRD, grad=0) == INV
 
 
+@pytest.mark.parametrize("fn,base,names", [
+    (fsb.fs_linear_device, LIN, ("M", "N", "K")), (fsb.fs_logprob_device, LGP, ("R", "C", "T", "K")),
+    (fsb.fs_distill_device, DST, ("R", "C", "K")), (fsb.fs_distill_grad_device, GRD, ("R", "C", "K")),
+])
+def test_numbers_that_do_not_fit_are_not_cut(fn, base, names):
+    # 2^32 + 2 rows are not two, and 2^32 are not none
+    for n in names:
+        for v in (1 << 31, 1 << 32, (1 << 32) + base[n], -(1 << 32) + base[n], -(1 << 31) - 1):
+            with pytest.raises(fsb.FsError) as e:
+                fn(*{**base, n: v}.values())
+            assert e.value.status == INV and "fit" in str(e.value)
+    for n in [k for k in base if k.startswith("ld")]:
+        with pytest.raises(fsb.FsError) as e:
+            fn(*{**base, n: (1 << 64) + base[n]}.values())
+        assert e.value.status == INV and "fit" in str(e.value)
+
+
 def test_valid_call_without_a_device_reports_it():
     import torch
     if torch.cuda.is_available():
