@@ -308,3 +308,23 @@ def test_more_than_the_caches_hold(gpu_lib, prec, R, C, K):
         near(c.entropy.numpy()[r:r + 1, 0], want["entropy"], lambda v: (128 + 48 * (1 + math.log(C))) * U)
     top = c.z.view.float().sort(dim=1, descending=True, stable=True)
     assert torch.equal(c.ids.view, top.indices[:, :K].int())
+
+
+@pytest.mark.parametrize("prec", [BF, F])
+@pytest.mark.parametrize("K", [1, 48, 49, 80])
+@pytest.mark.parametrize("kind", ["rising", "falling", "equal", "few", "steps", "late"])
+def test_hard_orders_by_one_and_two_waves_against_the_definition(gpu_lib, kind, K, prec):
+    # rows of one and of two waves (K beyond 48), the orders shifted from row to row
+    C, R = 9000, 4000
+    i = torch.arange(C, device="cuda", dtype=torch.float32)
+    z = {"rising": i / C * 40 - 20, "falling": -i / C * 40, "equal": torch.full((C,), 1.5, device="cuda"),
+         "few": torch.where(i % 1000 == 7, 3.0, 0.0), "steps": torch.floor(i / 700), "late": torch.where(i > C - 200, 5.0, 0.0)}[kind]
+    z = z[(torch.arange(C, device="cuda")[None] + 37 * torch.arange(R, device="cuda")[:, None]) % C]
+    c = Call(z, prec, 1, K).run()
+    at = [0, 1, 243, 1999, R - 1]
+    want = ref.logprob(c.z.view[at].float().cpu().numpy(), c.classes[at].cpu().numpy(), K)
+    assert np.array_equal(c.ids.numpy()[at], want["top_ids"])
+    near(c.logp.numpy()[at], want["logp"], lambda v: (128 + 8 * np.abs(v)) * U)
+    near(c.best.numpy()[at], want["top_logp"], lambda v: (128 + 8 * np.abs(v)) * U)
+    near(c.entropy.numpy()[at, 0], want["entropy"], lambda v: (128 + 48 * (1 + math.log(C))) * U)
+    assert torch.equal(c.ids.view, c.z.view.float().sort(dim=1, descending=True, stable=True).indices[:, :K].int())
