@@ -436,6 +436,279 @@ __global__ void __launch_bounds__(NW * 64) k_linear_stream(LinearArgs a) {
   finish4(a, om, on, s, bias, res);
 }
 
+// --------------------------------------------- few fp32 tiles of any alignment
+// A tile of 16 FN features x 16 FM rows; wave w takes K-tiles w, w + NW, ... of the
+// reduction (128 bytes a row) as k_linear_stream does, but through registers, so that
+// rows may lie at any element: whole lines of 8 rows a load, D K-tiles on their way, then
+// through LDS of the wave's own into MFMA order.  LDS serves a wave's accesses in order,
+// so one buffer a wave is enough and nothing waits for another wave before the end.
+template <int FM, int FN, int NW, int D>
+__global__ void __launch_bounds__(NW * 64) k_linear_wave(LinearArgs a) {
+  constexpr int KT = 32, P = 2 * (FM + FN), BUF = (FM + FN) * 16 * ROW;
+  static_assert(FM * FN * 1024 <= BUF, "a wave's sums fit where its operands were");
+  static_assert(FM * FN <= NW, "a block per wave");
+  static_assert(D % 2 == 0, "a K-tile's registers follow from its place in the loop");
+  __shared__ __attribute__((aligned(1024))) char lds[NW * BUF];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int tiles_n = (a.N + 16 * FN - 1) / (16 * FN);
+  const int n0 = blockIdx.x % tiles_n * (16 * FN), m0 = blockIdx.x / tiles_n * (16 * FM);
+  const float* const xb = static_cast<const float*>(a.x) + (int64_t)m0 * a.ldx;
+  const float* const wb = static_cast<const float*>(a.w) + (int64_t)n0 * a.ldw;
+
+  // load p: tile rows 8 p .. 8 p + 7 (w's rows first), lane l chunk l % 8 of row l / 8; rows
+  // that do not exist read the last one: they enter only outputs that do not exist
+  uint32_t off[P];
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    const int r = (p < 2 * FN ? p : p - 2 * FN) * 8 + (lane >> 3), last = (p < 2 * FN ? a.N - n0 : a.M - m0) - 1;
+    off[p] = (uint32_t)((min(r, last) * (p < 2 * FN ? a.ldw : a.ldx) + (lane & 7) * 4) * 4);
+  }
+  char* const own = lds + wave * BUF;
+  char* const put[2] = {own + (lane >> 3) * ROW + (((lane & 7) ^ swz(lane >> 3)) << 4),
+                        own + (8 + (lane >> 3)) * ROW + (((lane & 7) ^ swz(8 + (lane >> 3))) << 4)};
+  const int whole = a.K / KT, n = whole > wave ? (whole - wave - 1) / NW + 1 : 0;
+
+  const int om = m0 + wave / FN * 16 + (lane & 15), on = n0 + wave % FN * 16 + (lane >> 4) * 4;
+  const bool finishes = wave < FM * FN;
+  const Bias4 bias(a, finishes ? on : a.N);
+  const floatx4 res = residual4(a, finishes && on < a.N ? om : a.M, on);
+
+  u32x4 reg[D][P];
+  auto from = [&](int p, int k0) { return reinterpret_cast<const float*>(reinterpret_cast<const char*>((p < 2 * FN ? wb : xb) + k0) + off[p]); };
+  auto fetch = [&](int s, u32x4 (&to)[P]) {  // the wave's s-th K-tile
+#pragma unroll
+    for (int p = 0; p < P; ++p) to[p] = *reinterpret_cast<const u32x4_at4*>(from(p, (s * NW + wave) * KT));
+  };
+  floatx4 acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+  u32x4 w[2][2][FN], x[2][2][FM];
+  // a K-tile from registers to operands of set t
+  auto turn = [&](const u32x4 (&from)[P], auto t) {
+    __asm__ __volatile__("" ::: "memory");
+#pragma unroll
+    for (int p = 0; p < P; ++p) *reinterpret_cast<u32x4*>(put[p & 1] + (p >> 1) * 16 * ROW) = from[p];
+    __asm__ __volatile__("" ::: "memory");
+    const char* at = own + (lane & 15) * ROW;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int c = ((4 * h + ((lane >> 4 & 1) << 1 | lane >> 5)) ^ swz(lane & 15)) << 4;  // as in k_linear_stream
+#pragma unroll
+      for (int j = 0; j < FN; ++j) w[t][h][j] = *reinterpret_cast<const u32x4*>(at + j * 16 * ROW + c);
+#pragma unroll
+      for (int i = 0; i < FM; ++i) x[t][h][i] = *reinterpret_cast<const u32x4*>(at + (FN + i) * 16 * ROW + c);
+    }
+    __asm__ __volatile__("" ::: "memory");
+  };
+  auto mma = [&](auto t) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+          for (int j = 0; j < FN; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[t][h][j][e]), __uint_as_float(x[t][h][i][e]), acc[i][j], 0, 0, 0);
+  };
+
+#pragma unroll
+  for (int d = 0; d < D; ++d)
+    if (d < n) fetch(d, reg[d]);
+  if (n > 0) {
+    turn(reg[0], std::integral_constant<int, 0>{});
+    if (D < n) fetch(D, reg[0]);
+  }
+  for (int s = 0; s < n; s += D)
+    static_for<0, D>([&](auto d) {
+      constexpr int NEXT = (d + 1) % D;
+      if (s + d >= n) return;
+      if (s + d + 1 < n) {
+        turn(reg[NEXT], std::integral_constant<int, (d + 1) & 1>{});
+        if (s + d + 1 + D < n) fetch(s + d + 1 + D, reg[NEXT]);
+      }
+      __builtin_amdgcn_sched_barrier(0);  // the next K-tile is under way before the MFMAs
+      mma(std::integral_constant<int, d & 1>{});
+      __builtin_amdgcn_sched_barrier(0);
+    });
+
+  if (a.K % KT && wave == whole % NW) {  // the rest of the reduction
+#pragma unroll
+    for (int p = 0; p < P; ++p) reg[0][p] = piece(from(p, 0) - (lane & 7) * 4, whole * KT + (lane & 7) * 4, a.K);
+    turn(reg[0], std::integral_constant<int, 0>{});
+    mma(std::integral_constant<int, 0>{});
+  }
+  floatx4* const part = reinterpret_cast<floatx4*>(own);
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) part[(i * FN + j) * 64 + lane] = acc[i][j];
+  __syncthreads();
+  if (!finishes) return;
+  floatx4 s = reinterpret_cast<const floatx4*>(lds)[wave * 64 + lane];
+#pragma unroll
+  for (int q = 1; q < NW; ++q) s += reinterpret_cast<const floatx4*>(lds + q * BUF)[wave * 64 + lane];
+  finish4(a, om, on, s, bias, res);
+}
+
+// ------------------------------------------------- fp32 tiles of any alignment
+// A tile of 32 FM rows x 32 FN features by G groups of 2 x 2 waves.  Group g sums
+// K-tiles g, g + G, ... (128 bytes a row), each of its waves FM x FN blocks of 16 x 16 over
+// all of a K-tile.  Rows pass through registers, D K-tiles ahead, into one of two LDS
+// buffers (laid out as in lds_dma.hpp), so that they may lie at any element; a K-tile
+// costs one barrier, which the MFMAs on the second half of its operands cover.
+template <int FM, int FN, int G, int D>
+__global__ void __launch_bounds__(G * 256) k_linear_mid(LinearArgs a) {
+  constexpr int KT = 32, BM = 32 * FM, BN = 32 * FN, P = FM + FN, BUF = (BM + BN) * ROW;
+  __shared__ __attribute__((aligned(1024))) char lds[G * 2 * BUF];
+  static_assert((G - 1) * FM * FN * 4096 <= G * 2 * BUF, "the other groups' sums fit where the operands were");
+  static_assert(D % 2 == 0, "a K-tile's buffer and registers follow from its place in the loop");
+  const int tid = threadIdx.x & 255, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = wave >> 2, wm = wave >> 1 & 1, wn = wave & 1;
+
+  // tiles as in k_linear_tile: consecutive ones on one XCD, in groups of 8 tile rows
+  const int tiles_m = (a.M + BM - 1) / BM, tiles_n = (a.N + BN - 1) / BN;
+  const int id = xcd_remap(blockIdx.x, gridDim.x);
+  const int group = id / (8 * tiles_n), in = id - group * 8 * tiles_n;
+  const int rows = min(8, tiles_m - group * 8);
+  const int m0 = (group * 8 + in % rows) * BM, n0 = in / rows * BN;
+  const float* const xb = static_cast<const float*>(a.x) + (int64_t)m0 * a.ldx;
+  const float* const wb = static_cast<const float*>(a.w) + (int64_t)n0 * a.ldw;
+
+  // thread t, piece p: tile row 32 p + t / 8 (x's rows first), chunk t % 8; rows that do not
+  // exist read the last one: they enter only outputs that do not exist
+  const int prow = tid >> 3, kc = (tid & 7) * 4;
+  uint32_t off[P];
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    const int r = prow + (p < FM ? p : p - FM) * 32, last = (p < FM ? a.M - m0 : a.N - n0) - 1;
+    off[p] = (uint32_t)((min(r, last) * (p < FM ? a.ldx : a.ldw) + kc) * 4);
+  }
+  char* const own = lds + g * 2 * BUF;
+  char* const put = own + prow * ROW + (((tid & 7) ^ swz(prow)) << 4);
+  const int whole = a.K / KT, n = (whole + G - 1) / G;  // K-tiles, and those of a group (zeros behind the last)
+
+  u32x4 reg[D][P];
+  auto from = [&](int p, int k0) { return reinterpret_cast<const float*>(reinterpret_cast<const char*>((p < FM ? xb : wb) + k0) + off[p]); };
+  auto fetch = [&](int s, u32x4 (&to)[P]) {  // the group's s-th K-tile
+    if (G == 1 || s * G + g < whole) {       // the same for the whole wave
+#pragma unroll
+      for (int p = 0; p < P; ++p) to[p] = *reinterpret_cast<const u32x4_at4*>(from(p, (s * G + g) * KT));
+    } else {
+#pragma unroll
+      for (int p = 0; p < P; ++p) to[p] = u32x4{0, 0, 0, 0};
+    }
+  };
+  auto store = [&](int b, const u32x4 (&from)[P]) {
+#pragma unroll
+    for (int p = 0; p < P; ++p) *reinterpret_cast<u32x4*>(put + b * BUF + p * 32 * ROW) = from[p];
+  };
+  floatx4 acc[FM][FN];
+#pragma unroll
+  for (int i = 0; i < FM; ++i)
+#pragma unroll
+    for (int j = 0; j < FN; ++j) acc[i][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+
+  // half h of a K-tile's operands: lane groups 0, 1, 2, 3 take chunks 0, 2, 1, 3 of the half, as in k_linear_stream
+  u32x4 x[2][FM], w[2][FN];
+  const char* const at = own + (lane & 15) * ROW;
+  auto read = [&](int b, int h) {
+    const int c = ((4 * h + ((lane >> 4 & 1) << 1 | lane >> 5)) ^ swz(lane & 15)) << 4;
+#pragma unroll
+    for (int i = 0; i < FM; ++i) x[h][i] = *reinterpret_cast<const u32x4*>(at + b * BUF + (wm * FM + i) * 16 * ROW + c);
+#pragma unroll
+    for (int j = 0; j < FN; ++j) w[h][j] = *reinterpret_cast<const u32x4*>(at + b * BUF + (BM + (wn * FN + j) * 16) * ROW + c);
+  };
+  auto mma = [&](int h) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[h][j][e]), __uint_as_float(x[h][i][e]), acc[i][j], 0, 0, 0);
+  };
+  auto meet = [&] {
+    __asm__ __volatile__("" ::: "memory");
+    wait_lgkm0();  // this wave's part of the next K-tile is in LDS, its operands of this one in registers
+    wg_barrier();
+  };
+
+#pragma unroll
+  for (int d = 0; d < D; ++d)
+    if (d < n) fetch(d, reg[d]);
+  if (n > 0) {
+    store(0, reg[0]);
+    if (D < n) fetch(D, reg[0]);
+    meet();
+    read(0, 0);
+  }
+  for (int s = 0; s < n; s += D)
+    static_for<0, D>([&](auto d) {
+      constexpr int NEXT = (d + 1) % D;
+      if (s + d >= n) return;
+      read(d & 1, 1);
+      if (s + d + 1 < n) {
+        store((d + 1) & 1, reg[NEXT]);
+        if (s + d + 1 + D < n) fetch(s + d + 1 + D, reg[NEXT]);
+      }
+      __builtin_amdgcn_sched_barrier(0);  // reads and stores are under way before the MFMAs
+      mma(0);
+      __builtin_amdgcn_sched_barrier(0);
+      meet();
+      if (s + d + 1 < n) read((d + 1) & 1, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      mma(1);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+
+  if (a.K % KT) {  // the rest of the reduction, by the first group
+    if (G == 1 || g == 0) {
+#pragma unroll
+      for (int p = 0; p < P; ++p) reg[0][p] = piece(from(p, 0) - kc, whole * KT + kc, a.K);
+      store(n & 1, reg[0]);
+    }
+    meet();
+    if (G == 1 || g == 0) {
+      read(n & 1, 0);
+      read(n & 1, 1);
+      mma(0);
+      mma(1);
+    }
+  }
+  if constexpr (G > 1) {  // the groups' sums, in their order
+    floatx4* const part = reinterpret_cast<floatx4*>(lds) + (wave & 3) * 64 + lane;
+    __syncthreads();
+    if (g > 0) {
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) part[((g - 1) * FM * FN + i * FN + j) * 256] = acc[i][j];
+    }
+    __syncthreads();
+    if (g > 0) return;
+#pragma unroll
+    for (int q = 0; q < G - 1; ++q)
+#pragma unroll
+      for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] += part[(q * FM * FN + i * FN + j) * 256];
+  }
+  // block (i, j): lane l holds row l % 16 and features 4 (l / 16) ..
+#pragma unroll
+  for (int j = 0; j < FN; ++j) {
+    const int on = n0 + (wn * FN + j) * 16 + (lane >> 4) * 4, om = m0 + wm * FM * 16 + (lane & 15);
+    const Bias4 bias(a, on);
+    floatx4 res[FM];
+#pragma unroll
+    for (int i = 0; i < FM; ++i) res[i] = on < a.N ? residual4(a, om + i * 16, on) : floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < FM; ++i) finish4(a, om + i * 16, on, acc[i][j], bias, res[i]);
+  }
+}
+
 // -------------------------------------------------------------- many tiles
 // A tile of BM rows x BN features on WM x WN waves.  K-tiles of 128 bytes a row
 // lie in LDS as in lds_dma.hpp, NBUF of them in turn.  DMA: the loads write LDS
@@ -723,43 +996,51 @@ void stream(const LinearArgs& a, hipStream_t s) {
   hipLaunchKernelGGL((k_linear_stream<T, FM, NW, S>), dim3((unsigned)((a.N + 15) / 16)), dim3(NW * 64), 0, s, a);
 }
 
+template <int FM, int FN, int NW, int D>
+void waves(const LinearArgs& a, hipStream_t s) {
+  const int64_t tiles = (int64_t)((a.N + 16 * FN - 1) / (16 * FN)) * ((a.M + 16 * FM - 1) / (16 * FM));
+  hipLaunchKernelGGL((k_linear_wave<FM, FN, NW, D>), dim3((unsigned)tiles), dim3(NW * 64), 0, s, a);
+}
+
+template <int FM, int FN, int G, int D>
+void mid(const LinearArgs& a, hipStream_t s) {
+  const int64_t tiles = (int64_t)((a.N + 32 * FN - 1) / (32 * FN)) * ((a.M + 32 * FM - 1) / (32 * FM));
+  hipLaunchKernelGGL((k_linear_mid<FM, FN, G, D>), dim3((unsigned)tiles), dim3(G * 256), 0, s, a);
+}
+
 template <class T, int BM, int BN, int WM, int WN, bool DMA, int NBUF>
 void tile(const LinearArgs& a, hipStream_t s) {
   const int64_t tiles = (int64_t)((a.N + BN - 1) / BN) * ((a.M + BM - 1) / BM);
   hipLaunchKernelGGL((k_linear_tile<T, BM, BN, WM, WN, DMA, NBUF>), dim3((unsigned)tiles), dim3(WM * WN * 64), 0, s, a);
 }
 
-// The other kernels, and what a K-tile (128 bytes of a row) costs
+// The other kernels for bf16, and what a K-tile (128 bytes of a row) costs
 // one workgroup of each, in us: one / `fit` of them on a CU, measured at 128 to 4096
 // rows, 4096 features and K = 4096, and what a round of workgroups costs besides.
-// One row per kernel, by type and by how the loads go.
+// One row per kernel, by how the loads go.
 enum Kernel { FEW_16x16, FEW_32x16, FEW_32x32, FEW_64x32, TILE_64x64, TILE_64x128, TILE_128x128, TILE_256x128, TILE_256x256, KERNELS };
 struct Cost {
   int bm, bn, fit;
   float alone, full, round;
 };
 // Where a kernel is not built, its cost is 0.
-enum Loads { BF16_ODD, BF16_REGISTERS, BF16_LDS, F32_REGISTERS, F32_LDS };
-constexpr Cost COSTS[5][KERNELS] = {
-    // bf16, loads through registers, some rows between two words
+enum Loads { ODD, REGISTERS, LDS };
+constexpr Cost COSTS[3][KERNELS] = {
+    // loads through registers, some rows between two words
     {{16, 16, 2, .242f, .419f, 3.5f}, {32, 16, 2, .352f, .603f, 3.5f}, {32, 32, 2, .45f, .77f, 2.5f}, {64, 32, 2, .60f, 1.07f, 2.5f}, {64, 64, 4, 1.02f, 1.65f, 3.f}, {}, {128, 128, 2, 1.72f, 1.74f, 6.f}, {}, {256, 256, 1, 3.1f, 3.1f, 16.f}},
-    // bf16, loads through registers
+    // loads through registers
     {{16, 16, 2, .145f, .255f, 3.5f}, {32, 16, 2, .219f, .395f, 3.5f}, {32, 32, 2, .303f, .517f, 2.5f}, {64, 32, 2, .41f, .766f, 2.5f}, {64, 64, 4, .89f, 1.33f, 3.f}, {}, {128, 128, 2, 1.58f, 1.66f, 6.f}, {}, {256, 256, 1, 2.8f, 2.8f, 16.f}},
-    // bf16, loads into LDS
+    // loads into LDS
     {{16, 16, 2, .103f, .205f, 3.5f}, {32, 16, 2, .157f, .328f, 3.5f}, {32, 32, 2, .245f, .456f, 2.5f}, {64, 32, 2, .345f, .67f, 2.5f}, {64, 64, 2, .33f, .50f, 3.f}, {64, 128, 2, .44f, .74f, 4.f}, {128, 128, 2, .62f, 1.03f, 7.f}, {256, 128, 1, .94f, .94f, 9.f}, {256, 256, 1, 1.48f, 1.48f, 16.f}},
-    // fp32, loads through registers
-    {{16, 16, 2, .105f, .22f, 3.5f}, {32, 16, 2, .16f, .34f, 3.5f}, {32, 32, 2, .28f, .53f, 2.5f}, {64, 32, 2, .50f, .99f, 2.5f}, {64, 64, 2, 1.28f, 1.5f, 3.f}, {}, {128, 128, 2, 3.1f, 4.35f, 6.f}, {}, {256, 256, 1, 8.2f, 8.2f, 16.f}},
-    // fp32, loads into LDS: the matrix cores' rate, 7.4 us for 256 x 256 outputs
-    {{16, 16, 2, .105f, .22f, 3.5f}, {32, 16, 2, .16f, .34f, 3.5f}, {32, 32, 2, .277f, .53f, 2.5f}, {64, 32, 2, .50f, .97f, 2.5f}, {64, 64, 2, 1.15f, 1.22f, 3.f}, {64, 128, 2, 1.13f, 2.26f, 4.f}, {128, 128, 2, 2.06f, 3.95f, 6.f}, {256, 128, 1, 3.85f, 3.85f, 9.f}, {256, 256, 1, 7.45f, 7.45f, 16.f}},
 };
 
 // The kernel with the least time by those costs: whole rounds of the chip and the
-// rest.  (bf16, K = 4096: 512 x 4096 outputs 64 x 128 32 us against 36 for 64 x 64 and
+// rest.  (K = 4096: 512 x 4096 outputs 64 x 128 32 us against 36 for 64 x 64 and
 // 44 for 128 x 128; 1024 x 4096 128 x 128 45 against 66 and, 256 x 256, 86; 2048 x 4096
 // 256 x 128 69 against 75 and 91; 4096 x 4096 256 x 256 114 against 134 for 256 x 128; 41 x
 // 58, K = 18939, 16 x 16 89 before and 54 after shifting odd rows, 32 x 32 177.)
 Kernel pick(const LinearArgs& a, Loads loads, bool near, double* us) {
-  const int64_t steps = ((int64_t)a.K * (loads < F32_REGISTERS ? 2 : 4) + ROW - 1) / ROW;
+  const int64_t steps = ((int64_t)a.K * 2 + ROW - 1) / ROW;
   Kernel best = FEW_16x16;
   double least = 0;
   for (int k = 0; k < (near ? KERNELS : TILE_64x64); ++k) {
@@ -780,16 +1061,55 @@ Kernel pick(const LinearArgs& a, Loads loads, bool near, double* us) {
   return best;
 }
 
-// What k_linear_stream takes for blocks of 16 rows, in us: a workgroup brings 47 GB/s
-// from L2 (12 TB/s in all), up to 95 of bf16 where there are fewer of them, the chip 5.5
-// TB/s of weights from memory.  (4096 features, K = 4096, bf16: 16 rows 9.1 us,
+// The kernels for fp32: what a K-tile costs a workgroup alone on its CU and two of them,
+// what an output tile costs besides, in us, all measured with 16 to 2048 workgroups at K = 4096 and
+// 512.  `pairs`: two fit a CU, and one behind a pair takes as long as a pair.
+struct F32Cost {
+  int bm, bn;
+  float alone, two, tile;
+  bool pairs, dma;
+  void (*run)(const LinearArgs&, hipStream_t);
+};
+const F32Cost F32_COSTS[] = {
+    {16, 16, .085f, .147f, .9f, false, false, waves<1, 1, 8, 4>},   {32, 16, .155f, .25f, .95f, false, false, waves<2, 1, 8, 2>},
+    {32, 32, .2f, .335f, .9f, false, false, mid<1, 1, 4, 2>},       {32, 64, .336f, .6f, 1.1f, false, false, mid<1, 2, 2, 4>},
+    {64, 32, .336f, .6f, 1.1f, false, false, mid<2, 1, 2, 4>},      {64, 64, .57f, 1.12f, 1.9f, false, false, mid<2, 2, 2, 2>},
+    {64, 64, .665f, 1.07f, 1.45f, true, false, mid<2, 2, 1, 4>},    {64, 96, .955f, 1.5f, 3.f, true, false, mid<2, 3, 1, 4>},
+    {96, 64, .955f, 1.5f, 3.f, true, false, mid<3, 2, 1, 4>},       {96, 96, 1.355f, 2.2f, 4.5f, true, false, mid<3, 3, 1, 4>},
+    {64, 128, 1.235f, 1.975f, 4.5f, true, false, mid<2, 4, 1, 4>},  {128, 64, 1.235f, 1.975f, 4.5f, true, false, mid<4, 2, 1, 4>},
+    {128, 128, 2.1f, 3.8f, 4.9f, true, true, tile<float, 128, 128, 2, 2, true, 2>},
+    {256, 256, 7.45f, 14.9f, 24.f, false, true, tile<float, 256, 256, 2, 4, true, 2>},
+};
+
+// The one with the least time by those costs.  (580 x 1891 outputs, K = 4785, 32 x 32 130 us
+// against 155 for 64 x 64; 975 x 2986, K = 10274, 64 x 96 474 against 530 for 96 x 96 and 550 for 32 x 64; 1089 x
+// 1216, K = 4096, 32 x 64 111 against 121 for 96 x 64; 54 x 832, K = 5760, 16 x 16 14 against 22 for
+// 32 x 16 and 32 for 32 x 32; 4096 x 4096, K = 4096, 256 x 256 955, 64 x 128 1010, 64 x 64 1115.)
+const F32Cost& pick_f32(const LinearArgs& a, bool dma, double* us) {
+  const F32Cost* best = nullptr;
+  for (const F32Cost& c : F32_COSTS) {
+    if (c.dma && !dma) continue;
+    const int64_t n = ((a.M + c.bm - 1) / c.bm) * (int64_t)((a.N + c.bn - 1) / c.bn), steps = ((int64_t)a.K + 31) / 32;
+    const int64_t cu = (n + 255) / 256;  // of the CU with the most
+    const double t = 2.5 + cu * (double)c.tile + steps * (cu == 1 ? (double)c.alone : (c.pairs ? (cu + 1) / 2 * 2 : cu) * .5 * c.two);
+    if (!best || t < *us) {
+      best = &c;
+      *us = t;
+    }
+  }
+  return *best;
+}
+
+// What k_linear_stream takes for blocks of 16 rows, in us: the workgroups bring 12 TB/s from L2,
+// one of them up to 95 GB/s of bf16 and, of fp32, 97, 83 or 56 GB/s for one, two or more blocks; the chip
+// 5.5 TB/s of weights from memory.  (4096 features, K = 4096, bf16: 16 rows 9.1 us,
 // k_linear_few 10.1; 32 rows 10.9 and 14.3; 48 rows 12.7 and 17.5; 64 rows 14.3 and 18.3.
-// K = 25088: 32 rows 51 and 72, 64 rows 71 and 93.  48 x 64, K = 11136: 17 and 22; 54 x 832
-// fp32, K = 5760, 42 and 20.)
+// K = 25088: 32 rows 51 and 72, 64 rows 71 and 93.  48 x 64, K = 11136: 17 and 22.  fp32: 32 x 4096, K =
+// 4096, 20 and, k_linear_wave, 22; 64 x 4096, K = 25088, 180 and, k_linear_mid, 150; 64 x 1000, K = 4096, 25 and 16.)
 double stream_us(const LinearArgs& a, int blocks, int es) {
-  const double row = (double)a.K * es;
+  const double row = (double)a.K * es, one = es == 2 ? 95e3 : blocks == 1 ? 97e3 : blocks == 2 ? 83e3 : 56e3;
   const int groups = (a.N + 15) / 16, rounds = (groups + 255) / 256;
-  return 2. + std::max(rounds * (16. + 16. * blocks) * row / (es == 2 ? std::min(95e3, 12e6 / std::min(groups, 256)) : 47e3), a.N * row / 5.5e6);
+  return 2. + std::max(rounds * (16. + 16. * blocks) * row / std::min(one, 12e6 / std::min(groups, 256)), a.N * row / 5.5e6);
 }
 
 template <class T>
@@ -801,12 +1121,25 @@ void launch_t(const LinearArgs& a, hipStream_t s) {
                    reinterpret_cast<uintptr_t>(a.w) % 16 == 0;
   // a tile of 256 rows is addressed by 31-bit offsets from its first one
   const bool near = (255 * std::max(a.ldx, a.ldw) + a.K) * (int64_t)sizeof(T) < (int64_t(1) << 31);
-  // up to 8 rows the weights are all there is to read: 16 features a workgroup (4096
-  // features, K = 25088, bf16: 37 us for one row, 5.5 TB/s; with 8 waves 42)
-  if (a.M <= 8) return few<T, 1, 1, 16, 2>(a, s);
-  const Loads loads = F ? (dma ? F32_LDS : F32_REGISTERS) : dma ? BF16_LDS : odd_rows<T>(a) ? BF16_ODD : BF16_REGISTERS;
+  // up to 8 rows the weights are all there is to read.  k_linear_stream reads them for up to
+  // 2048 features and for rows of 32 KB and more (one row, bf16: 1000 features, K = 25088,
+  // 22 us against 30 with k_linear_few; 64 features 14 against 29; 4096 features 36 against 37; 8
+  // rows, fp32, 1000 features, K = 4096, 9.6 against 14.5), k_linear_wave fp32 rows that are not
+  // aligned (8 rows, 1000 features, K = 25088, 72 against 88), 16 features a workgroup of 16 waves
+  // the rest (one row, bf16: 4096 features, K = 4096, 7.9 against 8.4; 16384 features, K = 2048,
+  // 13.0 against 17.8; with 8 waves 4096 features, K = 25088, 42)
+  if (a.M <= 8) {
+    if (near && (a.N <= 2048 || a.K * (int64_t)sizeof(T) >= 32768)) {
+      if (dma) return stream<T, 1, 8, 3>(a, s);
+      if (F) return waves<1, 1, 8, 4>(a, s);
+    }
+    return few<T, 1, 1, 16, 2>(a, s);
+  }
   double us;
-  const Kernel k = pick(a, loads, near, &us);
+  const F32Cost* f = nullptr;
+  Kernel k = FEW_64x32;  // fp32 rows that are far apart
+  if (!F) k = pick(a, dma ? LDS : odd_rows<T>(a) ? ODD : REGISTERS, near, &us);
+  else if (near) f = &pick_f32(a, dma, &us);
   if (a.M <= 64 && dma && near) {
     const int blocks = (a.M + 15) / 16;
     if (stream_us(a, blocks, sizeof(T)) < us) {
@@ -816,16 +1149,21 @@ void launch_t(const LinearArgs& a, hipStream_t s) {
       return stream<T, 4, 4, 3>(a, s);
     }
   }
-  switch (k) {
-    case FEW_16x16: return few<T, 1, 1, 16, 2>(a, s);
-    case FEW_32x16: return few<T, 2, 1, 16, 2>(a, s);
-    case FEW_32x32: return few<T, 2, 2, 8, 2>(a, s);
-    case FEW_64x32: return few<T, 4, 2, 8, 1>(a, s);
-    case TILE_64x64: return dma ? tile<T, 64, 64, 1, 2, true, 4>(a, s) : tile<T, 64, 64, 2, 2, false, 2>(a, s);
-    case TILE_64x128: return tile<T, 64, 128, 1, 4, true, 3>(a, s);
-    case TILE_128x128: return dma ? tile<T, 128, 128, 2, 2, true, 2>(a, s) : tile<T, 128, 128, 2, 2, false, 2>(a, s);
-    case TILE_256x128: return tile<T, 256, 128, 2, 4, true, 3>(a, s);
-    default: return dma ? tile<T, 256, 256, 2, 4, true, 2>(a, s) : tile<T, 256, 256, 2, 4, false, 2>(a, s);
+  if (f) return f->run(a, s);
+  if constexpr (F) {
+    few<T, 4, 2, 8, 1>(a, s);
+  } else {
+    switch (k) {
+      case FEW_16x16: return few<T, 1, 1, 16, 2>(a, s);
+      case FEW_32x16: return few<T, 2, 1, 16, 2>(a, s);
+      case FEW_32x32: return few<T, 2, 2, 8, 2>(a, s);
+      case FEW_64x32: return few<T, 4, 2, 8, 1>(a, s);
+      case TILE_64x64: return dma ? tile<T, 64, 64, 1, 2, true, 4>(a, s) : tile<T, 64, 64, 2, 2, false, 2>(a, s);
+      case TILE_64x128: return tile<T, 64, 128, 1, 4, true, 3>(a, s);
+      case TILE_128x128: return dma ? tile<T, 128, 128, 2, 2, true, 2>(a, s) : tile<T, 128, 128, 2, 2, false, 2>(a, s);
+      case TILE_256x128: return tile<T, 256, 128, 2, 4, true, 3>(a, s);
+      default: return dma ? tile<T, 256, 256, 2, 4, true, 2>(a, s) : tile<T, 256, 256, 2, 4, false, 2>(a, s);
+    }
   }
 }
 

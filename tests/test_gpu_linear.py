@@ -299,3 +299,87 @@ def test_the_tails_of_the_activations(gpu_lib, M, out, act):
     steps = 16 * U if out == F else 16 * U + 3 * U * exponent + 2.0 ** -8
     off = np.abs(y.numpy().astype(np.float64) - want) - (steps * np.abs(want) + np.abs(s) * 2.0 ** -126)
     assert (off <= 0).all(), (off.max(), s[off.max(0).argmax()])
+
+
+@pytest.mark.parametrize("prec", [BF, F])
+@pytest.mark.parametrize("M,N,K", [(1, 2048, 4096), (8, 2049, 4096), (1, 33, 16384), (5, 2100, 8192), (8, 2064, 16376), (3, 1, 8), (7, 2048, 24)])
+def test_up_to_eight_rows_by_either_kernel(gpu_lib, M, N, K, prec):
+    x, w, b, r, y = make(M, N, K, prec, prec, True, pads=(8, 8, 3, 1), seed=14)
+    for t in (x, w):  # what lies beside the rows is read into no sum
+        keep = t.view.clone()
+        t.buf.fill_(float("nan"))
+        t.view.copy_(keep)
+    call(x, w, b, r, y, prec, prec, 2, 1)
+    check(x, w, b, r, y, prec, 2, 1)
+
+
+def against_64_bits_on_the_gpu(x, w, b, r, y, K, out):
+    xd, wd, rd = x.view.double(), w.view.double(), r.view.double()
+    want = xd @ wd.t() + b.double() + rd
+    size = xd.abs() @ wd.abs().t() + b.double().abs() + rd.abs()
+    half = 2.0 ** -8 if out == BF else U  # as in tolerance()
+    off = (y.view.double() - want).abs() - (1.13 * (min(2 * K, 160) + 24) * U * size + half * want.abs() + 1e-37)
+    assert bool((off <= 0).all()), (float(off.max()), int(off.argmax()) // y.cols, int(off.argmax()) % y.cols)
+    assert y.untouched()
+
+
+@pytest.mark.parametrize("pad,lead", [(0, 0), (3, 0), (8, 1)])
+@pytest.mark.parametrize("M,N,K", [
+    (45, 65, 2463), (9, 17, 31), (1398, 33, 100), (65, 1407, 68), (1347, 164, 100), (1345, 321, 68), (322, 1481, 260), (322, 1481, 257),
+    (386, 1222, 5), (1475, 322, 68), (1154, 842, 36), (1346, 1060, 36), (1409, 1415, 68), (1000, 4090, 1030), (4200, 955, 2052),
+    (2000, 4090, 520), (4000, 4090, 2056), (33, 64, 32), (64, 33, 96), (130, 97, 3),
+])
+def test_every_tile_of_fp32(gpu_lib, M, N, K, pad, lead):
+    # ragged edges, the reduction's last part, rows at any element; what lies beside the rows is read into no sum
+    x, w, b, r, y = make(M, N, K, F, F, True, pads=(pad, pad, pad, 1), leads=(lead, lead, lead, 0), seed=15)
+    for t in (x, w):
+        keep = t.view.clone()
+        t.buf.fill_(float("nan"))
+        t.view.copy_(keep)
+    call(x, w, b, r, y, F, F, 0, 1)
+    against_64_bits_on_the_gpu(x, w, b, r, y, K, F)
+    first = y.view.clone()
+    call(x, w, b, r, y, F, F, 0, 1)
+    assert torch.equal(y.view, first)
+    call(x, w, b, r, r, F, F, 0, 1)  # over the residual
+    assert torch.equal(r.view, first) and r.untouched()
+
+
+@pytest.mark.parametrize("M,N,K", [(40, 70, 1000), (70, 1407, 260), (400, 1400, 100), (1154, 842, 37)])
+def test_fp32_values_that_are_not_finite_stay_in_their_rows(gpu_lib, M, N, K):
+    x, w, b, r, y = make(M, N, K, F, F, True, pads=(1, 3, 0, 0), seed=16)
+    x.view[1, K - 1] = float("nan")
+    w.view[2, 0] = float("inf")
+    call(x, w, b, r, y, F, F, 0, 1)
+    assert bool(y.view[1].isnan().all()) and not bool(y.view[:, 2].isfinite().any())
+    x.view[1], w.view[2] = 0, 0
+    y.view[1], y.view[:, 2] = b + r.view[1], b[2] + r.view[:, 2]
+    against_64_bits_on_the_gpu(x, w, b, r, y, K, F)
+
+
+def test_fp32_rows_that_are_far_apart(gpu_lib):
+    # rows 2^22 elements apart: more than a tile's offsets reach, and beyond 2^31 bytes in all
+    far = (1 << 22) + 1
+    for M, N in ((150, 70), (70, 150), (5, 150), (150, 5)):
+        x, w = torch.randn(M, 67, device="cuda"), torch.randn(N, 67, device="cuda")
+        big = torch.empty(150 * far, device="cuda")
+        v = big.view(150, far)[:, :67]
+        v.copy_(x if M == 150 else w)
+        y = Rows(M, N, torch.float32)
+        px, lx, pw, lw = ((v.data_ptr(), far, w.data_ptr(), 67) if M == 150 else (x.data_ptr(), 67, v.data_ptr(), far))
+        fsb.fs_linear_device(px, lx, pw, lw, 0, 0, 0, y.ptr, y.ld, M, N, 67, F, F, 0, 0, stream())
+        want, size = ref.linear(x.cpu().numpy(), w.cpu().numpy())
+        assert (np.abs(y.numpy() - want) <= tolerance(want, size, 67, F)).all()
+        del big, v
+
+
+@pytest.mark.parametrize("M,N", [(12, (1 << 24) + 5), ((1 << 26), 5)])
+def test_more_fp32_outputs_than_a_launch_has_threads(gpu_lib, M, N):
+    x, w, b, r, y = make(M, N, 1, F, F, False, seed=17)  # one product and one addition per output
+    call(x, w, b, None, y, F, F, 0, 0)
+    for m in range(0, M, 1 << 24):
+        rows = slice(m, m + (1 << 24))
+        want = (x.view[rows].double() * w.view.double().t() + b.double())
+        off = (y.view[rows].double() - want).abs() - 2 * U * (want.abs() + b.double().abs())
+        assert bool((off <= 0).all())
+    assert bool((y.buf[-64:] == MARK).all())
