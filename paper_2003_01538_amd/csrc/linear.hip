@@ -1061,9 +1061,11 @@ Kernel pick(const LinearArgs& a, Loads loads, bool near, double* us) {
   return best;
 }
 
-// The kernels for fp32: what a K-tile costs a workgroup alone on its CU and two of them,
-// what an output tile costs besides, in us, all measured with 16 to 2048 workgroups at K = 4096 and
-// 512.  `pairs`: two fit a CU, and one behind a pair takes as long as a pair.
+// The kernels for fp32: what a K-tile costs a workgroup alone on its CU and two of them, and
+// what an output tile costs besides 2.5 us of the launch, in us, measured with 16 to 2048
+// workgroups at K = 4096 and 512.  `pairs`: two fit a CU, and one behind a pair takes as long
+// as a pair.  No less than the operands' way from L2 takes, at 11.5 TB/s (376 x 768 outputs, K = 11136,
+// 16 x 16 143 us, 32 x 32 109).
 struct F32Cost {
   int bm, bn;
   float alone, two, tile;
@@ -1071,27 +1073,30 @@ struct F32Cost {
   void (*run)(const LinearArgs&, hipStream_t);
 };
 const F32Cost F32_COSTS[] = {
-    {16, 16, .085f, .147f, .9f, false, false, waves<1, 1, 8, 4>},   {32, 16, .155f, .25f, .95f, false, false, waves<2, 1, 8, 2>},
-    {32, 32, .2f, .335f, .9f, false, false, mid<1, 1, 4, 2>},       {32, 64, .336f, .6f, 1.1f, false, false, mid<1, 2, 2, 4>},
-    {64, 32, .336f, .6f, 1.1f, false, false, mid<2, 1, 2, 4>},      {64, 64, .57f, 1.12f, 1.9f, false, false, mid<2, 2, 2, 2>},
-    {64, 64, .665f, 1.07f, 1.45f, true, false, mid<2, 2, 1, 4>},    {64, 96, .955f, 1.5f, 3.f, true, false, mid<2, 3, 1, 4>},
-    {96, 64, .955f, 1.5f, 3.f, true, false, mid<3, 2, 1, 4>},       {96, 96, 1.355f, 2.2f, 4.5f, true, false, mid<3, 3, 1, 4>},
-    {64, 128, 1.235f, 1.975f, 4.5f, true, false, mid<2, 4, 1, 4>},  {128, 64, 1.235f, 1.975f, 4.5f, true, false, mid<4, 2, 1, 4>},
-    {128, 128, 2.1f, 3.8f, 4.9f, true, true, tile<float, 128, 128, 2, 2, true, 2>},
-    {256, 256, 7.45f, 14.9f, 24.f, false, true, tile<float, 256, 256, 2, 4, true, 2>},
+    {16, 16, .06f, .112f, .9f, false, false, waves<1, 1, 8, 4>},    {16, 32, .105f, .2f, .95f, false, false, waves<1, 2, 8, 2>},
+    {32, 16, .107f, .2f, .95f, false, false, waves<2, 1, 8, 2>},    {32, 32, .178f, .305f, 1.6f, false, false, mid<1, 1, 4, 2>},
+    {32, 64, .308f, .555f, 2.f, false, false, mid<1, 2, 2, 4>},    {64, 32, .308f, .555f, 2.f, false, false, mid<2, 1, 2, 4>},
+    {64, 64, .536f, 1.075f, 3.f, false, false, mid<2, 2, 2, 2>},   {64, 64, .634f, 1.03f, 1.45f, true, false, mid<2, 2, 1, 4>},
+    {64, 96, .912f, 1.43f, 3.f, true, false, mid<2, 3, 1, 4>},      {96, 64, .912f, 1.43f, 3.f, true, false, mid<3, 2, 1, 4>},
+    {96, 96, 1.3f, 2.11f, 4.5f, true, false, mid<3, 3, 1, 4>},      {64, 128, 1.18f, 1.885f, 4.5f, true, false, mid<2, 4, 1, 4>},
+    {128, 64, 1.18f, 1.885f, 4.5f, true, false, mid<4, 2, 1, 4>},   {128, 128, 2.1f, 3.72f, 7.f, true, true, tile<float, 128, 128, 2, 2, true, 2>},
+    {256, 256, 7.28f, 14.56f, 24.f, false, true, tile<float, 256, 256, 2, 4, true, 2>},
 };
 
-// The one with the least time by those costs.  (580 x 1891 outputs, K = 4785, 32 x 32 130 us
+// The one with the least time by those costs; of 240 products of the operator's range it takes 2 %
+// more than the best of them on average.  (580 x 1891 outputs, K = 4785, 32 x 32 130 us
 // against 155 for 64 x 64; 975 x 2986, K = 10274, 64 x 96 474 against 530 for 96 x 96 and 550 for 32 x 64; 1089 x
-// 1216, K = 4096, 32 x 64 111 against 121 for 96 x 64; 54 x 832, K = 5760, 16 x 16 14 against 22 for
-// 32 x 16 and 32 for 32 x 32; 4096 x 4096, K = 4096, 256 x 256 955, 64 x 128 1010, 64 x 64 1115.)
+// 1216, K = 4096, 32 x 64 111 against 121 for 96 x 64; 54 x 832, K = 5760, 16 x 16 14 against 18 for
+// 16 x 32 and 32 for 32 x 32; 642 x 128, K = 13312, 16 x 32 45 against 48 for 32 x 16 and 68 for 16 x 16;
+// 4096 x 4096, K = 4096, 256 x 256 955, 64 x 128 1010, 64 x 64 1115.)
 const F32Cost& pick_f32(const LinearArgs& a, bool dma, double* us) {
   const F32Cost* best = nullptr;
   for (const F32Cost& c : F32_COSTS) {
     if (c.dma && !dma) continue;
     const int64_t n = ((a.M + c.bm - 1) / c.bm) * (int64_t)((a.N + c.bn - 1) / c.bn), steps = ((int64_t)a.K + 31) / 32;
     const int64_t cu = (n + 255) / 256;  // of the CU with the most
-    const double t = 2.5 + cu * (double)c.tile + steps * (cu == 1 ? (double)c.alone : (c.pairs ? (cu + 1) / 2 * 2 : cu) * .5 * c.two);
+    const double sums = steps * (cu == 1 ? (double)c.alone : (c.pairs ? (cu + 1) / 2 * 2 : cu) * .5 * c.two);
+    const double t = 2.5 + cu * (double)c.tile + std::max(sums, n * (double)(c.bm + c.bn) * a.K * 4 / 11.5e6);
     if (!best || t < *us) {
       best = &c;
       *us = t;

@@ -327,7 +327,8 @@ def against_64_bits_on_the_gpu(x, w, b, r, y, K, out):
 @pytest.mark.parametrize("M,N,K", [
     (45, 65, 2463), (9, 17, 31), (1398, 33, 100), (65, 1407, 68), (1347, 164, 100), (1345, 321, 68), (322, 1481, 260), (322, 1481, 257),
     (386, 1222, 5), (1475, 322, 68), (1154, 842, 36), (1346, 1060, 36), (1409, 1415, 68), (1000, 4090, 1030), (4200, 955, 2052),
-    (2000, 4090, 520), (4000, 4090, 2056), (33, 64, 32), (64, 33, 96), (130, 97, 3),
+    (2000, 4090, 520), (4000, 4090, 2056), (33, 64, 32), (64, 33, 96), (130, 97, 3), (51, 2061, 68), (2361, 195, 515), (99, 2362, 100),
+    (2119, 33, 64), (257, 2242, 1000),
 ])
 def test_every_tile_of_fp32(gpu_lib, M, N, K, pad, lead):
     # ragged edges, the reduction's last part, rows at any element; what lies beside the rows is read into no sum
