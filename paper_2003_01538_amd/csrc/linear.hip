@@ -1073,7 +1073,7 @@ struct F32Cost {
   void (*run)(const LinearArgs&, hipStream_t);
 };
 const F32Cost F32_COSTS[] = {
-    {16, 16, .06f, .112f, .9f, false, false, waves<1, 1, 8, 4>},    {16, 32, .105f, .2f, .95f, false, false, waves<1, 2, 8, 2>},
+    {16, 16, .06f, .112f, .9f, false, false, waves<1, 1, 12, 2>},   {16, 32, .105f, .2f, .95f, false, false, waves<1, 2, 8, 2>},
     {32, 16, .107f, .2f, .95f, false, false, waves<2, 1, 8, 2>},    {32, 32, .178f, .305f, 1.6f, false, false, mid<1, 1, 4, 2>},
     {32, 64, .308f, .555f, 2.f, false, false, mid<1, 2, 2, 4>},    {64, 32, .308f, .555f, 2.f, false, false, mid<2, 1, 2, 4>},
     {64, 64, .536f, 1.075f, 3.f, false, false, mid<2, 2, 2, 2>},   {64, 64, .634f, 1.03f, 1.45f, true, false, mid<2, 2, 1, 4>},
@@ -1129,16 +1129,15 @@ void launch_t(const LinearArgs& a, hipStream_t s) {
   // up to 8 rows the weights are all there is to read.  k_linear_stream reads them for up to
   // 2048 features and for rows of 32 KB and more (one row, bf16: 1000 features, K = 25088,
   // 22 us against 30 with k_linear_few; 64 features 14 against 29; 4096 features 36 against 37; 8
-  // rows, fp32, 1000 features, K = 4096, 9.6 against 14.5), k_linear_wave fp32 rows that are not
-  // aligned (8 rows, 1000 features, K = 25088, 72 against 88), 16 features a workgroup of 16 waves
-  // the rest (one row, bf16: 4096 features, K = 4096, 7.9 against 8.4; 16384 features, K = 2048,
-  // 13.0 against 17.8; with 8 waves 4096 features, K = 25088, 42)
+  // rows, fp32, 1000 features, K = 4096, 9.6 against 14.5), fp32 that it cannot take goes by costs up
+  // to 2048 features and for rows of 16 KB and more (rows 3 elements apart: one row of 1000, K = 25088, 53
+  // against 67, 8 of 5000, K = 4096, 24 against 30, but one of 16384, K = 1024, 18 against 15), and
+  // 16 features a workgroup of 16 waves take the rest (one row, bf16: 4096 features, K = 4096, 7.9
+  // against 8.4; 16384 features, K = 2048, 13.0 against 17.8; with 8 waves 4096 features, K = 25088, 42)
   if (a.M <= 8) {
-    if (near && (a.N <= 2048 || a.K * (int64_t)sizeof(T) >= 32768)) {
-      if (dma) return stream<T, 1, 8, 3>(a, s);
-      if (F) return waves<1, 1, 8, 4>(a, s);
-    }
-    return few<T, 1, 1, 16, 2>(a, s);
+    const int64_t row = a.K * (int64_t)sizeof(T);
+    if (near && dma && (a.N <= 2048 || row >= 32768)) return stream<T, 1, 8, 3>(a, s);
+    if (!F || !near || dma || (a.N > 2048 && row < 16384)) return few<T, 1, 1, 16, 2>(a, s);
   }
   double us;
   const F32Cost* f = nullptr;

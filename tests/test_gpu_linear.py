@@ -302,9 +302,11 @@ def test_the_tails_of_the_activations(gpu_lib, M, out, act):
 
 
 @pytest.mark.parametrize("prec", [BF, F])
-@pytest.mark.parametrize("M,N,K", [(1, 2048, 4096), (8, 2049, 4096), (1, 33, 16384), (5, 2100, 8192), (8, 2064, 16376), (3, 1, 8), (7, 2048, 24)])
-def test_up_to_eight_rows_by_either_kernel(gpu_lib, M, N, K, prec):
-    x, w, b, r, y = make(M, N, K, prec, prec, True, pads=(8, 8, 3, 1), seed=14)
+@pytest.mark.parametrize("pad", [8, 3])
+@pytest.mark.parametrize("M,N,K", [(1, 2048, 4096), (8, 2049, 4096), (1, 33, 16384), (5, 2100, 8192), (8, 2064, 16376), (3, 1, 8), (7, 2048, 24),
+                                   (6, 5000, 4099), (1, 2049, 4095), (8, 16, 25087)])
+def test_up_to_eight_rows_by_either_kernel(gpu_lib, M, N, K, pad, prec):
+    x, w, b, r, y = make(M, N, K, prec, prec, True, pads=(pad, pad, 3, 1), seed=14)
     for t in (x, w):  # what lies beside the rows is read into no sum
         keep = t.view.clone()
         t.buf.fill_(float("nan"))
