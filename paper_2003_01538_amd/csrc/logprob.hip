@@ -449,9 +449,11 @@ void launch_t(const LogprobArgs& a, hipStream_t s) {
   // rest (fp32: 96 rows of 1000, K = 5, 4.8 us against 5.4 with two waves; 60000 of 2049, K = 16,
   // 151 against 205 and, with four, 338; 8000 of 32768 199 against 209 and 221; 16000 of 1000 at K = 41
   // 35 against 61, at K = 64 158 against 66), with no more logits a thread than the row has
-  // (300000 rows of 100 218 us with 4, 370 with 16)
+  // (300000 rows of 100 218 us with 4, 370 with 16;
+  // also for more alternatives where there are many rows: 300000 of 100 at K = 64 368 us against 914 with
+  // two waves of 16 logits, at K = 128 383 against 1763 with four; 1000 of 250 at K = 64 18 against 13)
+  if (a.C <= 64 * VEC && (a.K <= 48 || a.R >= 4000)) return whole<T, 64, 1>(a, s);
   if (a.K <= 48) {
-    if (a.C <= 64 * VEC) return whole<T, 64, 1>(a, s);
     if (a.C <= 128 * VEC && NV > 2) return whole<T, 64, 2>(a, s);
     if (a.C <= 2048 || a.R >= 4000) return whole<T, 64, NV>(a, s);
   }

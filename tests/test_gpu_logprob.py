@@ -328,3 +328,24 @@ def test_hard_orders_by_one_and_two_waves_against_the_definition(gpu_lib, kind, 
     near(c.best.numpy()[at], want["top_logp"], lambda v: (128 + 8 * np.abs(v)) * U)
     near(c.entropy.numpy()[at, 0], want["entropy"], lambda v: (128 + 48 * (1 + math.log(C))) * U)
     assert torch.equal(c.ids.view, c.z.view.float().sort(dim=1, descending=True, stable=True).indices[:, :K].int())
+
+
+@pytest.mark.parametrize("prec", [BF, F])
+@pytest.mark.parametrize("C", [37, 100, 255, 256, 257, 511, 512, 513])
+@pytest.mark.parametrize("K", [49, 81, 128])
+def test_many_short_rows_with_many_alternatives(gpu_lib, C, K, prec):
+    z = logits(4100, C, 17)
+    z[:50] = torch.floor(z[:50])  # ties
+    z[50:60, C // 3:] = -float("inf")
+    z[60:64] = 1.0
+    c = Call(z, prec, 2, K, pad=C % 3).run()
+    at = [0, 7, 49, 50, 59, 60, 64, 2000, 4099]
+    want = ref.logprob(c.z.view[at].float().cpu().numpy(), c.classes[at].cpu().numpy(), K)
+    assert np.array_equal(c.ids.numpy()[at], want["top_ids"])
+    near(c.logp.numpy()[at], want["logp"], lambda v: (128 + 8 * np.abs(v)) * U)
+    near(c.best.numpy()[at], want["top_logp"], lambda v: (128 + 8 * np.abs(v)) * U)
+    near(c.entropy.numpy()[at, 0], want["entropy"], lambda v: (128 + 48 * (1 + math.log(C))) * U)
+    v, i = c.z.view.float().sort(dim=1, descending=True, stable=True)
+    n = min(K, C)
+    assert torch.equal(c.ids.view[:, :n], torch.where(v == -float("inf"), -1, i)[:, :n].int())
+    assert bool((c.ids.view[:, n:] == -1).all()) and all(t.untouched() for t in (c.logp, c.entropy, c.ids, c.best))
