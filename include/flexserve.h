@@ -463,7 +463,8 @@ typedef enum { FS_ACT_NONE = 0, FS_ACT_RELU = 1, FS_ACT_GELU = 2, FS_ACT_SILU = 
  *   d_y    [M][N], rows ldy apart; may be d_res with the same row distance
  * precision is the type of x and w, out_precision that of y and res: FS_F32,
  * or FS_BF16 for bf16 x and w.  Sums, bias, activation and residual are fp32
- * and rounded once.  K = 0 is an empty sum.
+ * and rounded once.  K = 0 is an empty sum.  The forward product only: a
+ * layer's gradients reduce over rows, which lie ldx and ldy apart here.
  * FS_ERR_INVALID for NULL, negative sizes or rows that are too near;
  * FS_ERR_UNSUPPORTED for bf16 output of fp32 inputs, M or N beyond 2^26, K
  * beyond 2^30. */

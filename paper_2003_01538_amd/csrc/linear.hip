@@ -1,21 +1,26 @@
 // Matrix product with bias, activation and residual on a caller's tensors:
 // y[m][n] = act(sum_k x[m][k] w[n][k] + bias[n] (+ res)) (+ res).
 //
-// Three kernels.  k_linear_few is for outputs of few tiles: a workgroup makes a
+// Five kernels.  k_linear_few is for outputs of few tiles: a workgroup makes a
 // small tile, 16 x 16 to 64 x 32, and its waves split the reduction, each loading its operands
 // straight into registers (nothing is shared, so nothing is staged), and their
 // sums meet in LDS in wave order.  k_linear_stream is its form for up to 64 aligned
 // rows.  k_linear_tile is for many tiles: operands go through LDS, each wave sums
-// its part of the tile over the whole reduction.  Rows may lie at any distance and
-// alignment; which kernel runs, with which tile, is a rule on sizes and alignment
-// (launch_t).
+// its part of the tile over the whole reduction.  fp32, whose matrix instructions take
+// eight times as long, has two of its own besides, which bring whole lines through
+// registers and LDS: k_linear_wave for few tiles, k_linear_mid for tiles of 32 x 32 to 128 x 64.
+// Rows may lie at any distance and alignment; which kernel runs, with which tile, is a rule on
+// sizes and alignment (launch_t).
 //
 // What bounds them: up to 16 rows the weights' way from memory (4096 features, K =
 // 25088, bf16, one row 37 us, 5.5 TB/s); up to 64 rows that of x from L2 to every
 // workgroup (32 rows 51 us, 12 TB/s); bf16 products of 4096 x 8192 x 4096 the power
-// that the matrix cores may take (216 to 222 us, 1.24 to 1.27 PFLOP/s, with their pipes
-// busy 73 % of the time at 1.7 GHz; the vendor's library 180 us; 240 us with GELU and
-// residual); fp32 products the matrix cores' rate (4096^3 953 us, 144 TFLOP/s).
+// that the matrix cores may take (216 to 229 us, 1.20 to 1.27 PFLOP/s, with their pipes
+// busy 73 % of the time at 1.7 GHz; the vendor's library 180 to 189 us; 238 to 256 us with GELU and
+// residual); fp32 products the matrix cores' rate (4096^3 947 us, 145 TFLOP/s; rows 3 elements
+// apart 1010 to 1041 us), mid-sized ones the rest of the last round of tiles (580 x 1891, K = 4785, 130
+// us, 81 TFLOP/s), long reductions over few outputs what a CU brings from L2, 50 to 100 GB/s
+// (74 x 128, K = 18816, 28 us).
 //
 // MFMA operands: A = weights, B = x, so that a lane's accumulators hold
 // consecutive features n of one row m.  The order of k inside a 16-byte piece
@@ -1094,6 +1099,7 @@ const F32Cost& pick_f32(const LinearArgs& a, bool dma, double* us) {
   for (const F32Cost& c : F32_COSTS) {
     if (c.dma && !dma) continue;
     const int64_t n = ((a.M + c.bm - 1) / c.bm) * (int64_t)((a.N + c.bn - 1) / c.bn), steps = ((int64_t)a.K + 31) / 32;
+    if (n >= 1 << 22) continue;          // of up to 1024 threads each: fewer than 2^32
     const int64_t cu = (n + 255) / 256;  // of the CU with the most
     const double sums = steps * (cu == 1 ? (double)c.alone : (c.pairs ? (cu + 1) / 2 * 2 : cu) * .5 * c.two);
     const double t = 2.5 + cu * (double)c.tile + std::max(sums, n * (double)(c.bm + c.bn) * a.K * 4 / 11.5e6);
@@ -1175,7 +1181,8 @@ void launch_t(const LinearArgs& a, hipStream_t s) {
 
 void launch_linear(const LinearArgs& a, Prec p, hipStream_t s) {
   // A launch has fewer than 2^32 threads, of which k_linear_few gives 64 to a feature or
-  // one to two outputs: products beyond go in slices.
+  // one to two outputs: products beyond go in slices (of at most 2^32 outputs, so that the larger
+  // of F32_COSTS have fewer than 2^22 tiles).
   constexpr int FEATURES = 1 << 24;
   const int64_t rows = (int64_t(1) << 32) / std::min(a.N, FEATURES) / 256 * 256;
   const int64_t ei = p == BF16 ? 2 : 4, eo = a.out_f32 ? 4 : 2;

@@ -21,7 +21,10 @@
 // segments' statistics and K best go to the scratch memory, and a second launch
 // joins them with the same selection.
 //
-// What bounds it: memory for many rows (2048 x 131072 fp32, K = 20, 188 us, 5.7 TB/s);
+// What bounds it: memory for many long rows (2048 x 131072 fp32, K = 20, 188 us, 5.7 TB/s),
+// the vector ALU for those of bf16 (8000 x 32768 170 to 178 us, 2.9 to 3.1 TB/s), a row's own steps for
+// many short ones (100000 x 1000, K = 5, 128 to 135 us in both types; 300000 x 100 223 us), the counting
+// of the list for many alternatives (16000 x 1000 fp32, K = 64, 65 us, K = 128 144 us);
 // for few the chain of loads, reductions and selection of a workgroup, two of them when
 // rows are split (one row of 131072 6.2 + 5.1 us).
 #include "rows.hpp"
@@ -449,9 +452,9 @@ void launch_t(const LogprobArgs& a, hipStream_t s) {
   // rest (fp32: 96 rows of 1000, K = 5, 4.8 us against 5.4 with two waves; 60000 of 2049, K = 16,
   // 151 against 205 and, with four, 338; 8000 of 32768 199 against 209 and 221; 16000 of 1000 at K = 41
   // 35 against 61, at K = 64 158 against 66), with no more logits a thread than the row has
-  // (300000 rows of 100 218 us with 4, 370 with 16;
-  // also for more alternatives where there are many rows: 300000 of 100 at K = 64 368 us against 914 with
-  // two waves of 16 logits, at K = 128 383 against 1763 with four; 1000 of 250 at K = 64 18 against 13)
+  // (300000 rows of 100 218 us with 4, 370 with 16).  Many rows that fit it with 4 go so for any K
+  // (300000 of 100 at K = 64 368 us against 914 with two waves of 16 logits, at K = 128 383 against 1763
+  // with four; 1000 of 250 at K = 64 18 against 13).
   if (a.C <= 64 * VEC && (a.K <= 48 || a.R >= 4000)) return whole<T, 64, 1>(a, s);
   if (a.K <= 48) {
     if (a.C <= 128 * VEC && NV > 2) return whole<T, 64, 2>(a, s);
