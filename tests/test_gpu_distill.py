@@ -341,20 +341,21 @@ def test_one_waves_gradient_past_the_caches(gpu_lib, prec, R, C, K):
     past_the_caches(R, C, K, prec, False)
 
 
-# vectors of 16 bytes that a row's threads hold, where the next larger kernel begins
-HELD = [64 * 4, 128 * 4, 128 * 6, 256 * 4, 256 * 6, 256 * 8, 256 * 10, 256 * 12, 256 * 14, 256 * 16, 512 * 10, 512 * 12, 512 * 14,
-        512 * 16, 512 * 20, 512 * 24, 512 * 28, 512 * 32]
+# threads and the vectors of 16 bytes that each holds of a row, where the next larger kernel begins
+HELD = [(64, 4), (128, 4), (128, 6), (256, 4), (256, 6), (256, 8), (256, 10), (256, 12), (256, 14), (256, 16), (512, 10), (512, 12),
+        (512, 14), (512, 16), (512, 20), (512, 24), (512, 28), (512, 32)]
 
 
 @pytest.mark.parametrize("prec", [BF, F])
-@pytest.mark.parametrize("vectors", HELD)
-def test_rows_that_just_fit_a_workgroup(gpu_lib, vectors, prec):
-    for C in (vectors * (8 if prec == BF else 4), vectors * (8 if prec == BF else 4) - 3):
+@pytest.mark.parametrize("threads,held", HELD)
+def test_rows_that_just_fit_a_workgroup(gpu_lib, threads, held, prec):
+    most = threads * held * (8 if prec == BF else 4)
+    for C in [most - 1, most - 3] + ([most] if held in (4, 16, 32) else []):
         Call(*inputs(3, C, 11), prec, 2.0, split=False).run().check_loss().check_grad()
 
 
 @pytest.mark.parametrize("prec", [BF, F])
-@pytest.mark.parametrize("vectors", HELD[4:])
-def test_rows_that_just_fit_a_workgroup_past_the_caches(gpu_lib, vectors, prec):
-    C, es = vectors * (8 if prec == BF else 4) - vectors // 512 % 2, 2 if prec == BF else 4
+@pytest.mark.parametrize("threads,held", HELD[4:])
+def test_rows_that_just_fit_a_workgroup_past_the_caches(gpu_lib, threads, held, prec):
+    C, es = threads * held * (8 if prec == BF else 4) - held // 2 % 2, 2 if prec == BF else 4
     past_the_caches((400 << 20) // (2 * C * es) + 9, C, 11, prec, True)

@@ -386,3 +386,31 @@ def test_more_fp32_outputs_than_a_launch_has_threads(gpu_lib, M, N):
         off = (y.view[rows].double() - want).abs() - 2 * U * (want.abs() + b.double().abs())
         assert bool((off <= 0).all())
     assert bool((y.buf[-64:] == MARK).all())
+
+
+@pytest.mark.parametrize("M,N,K", [(45, 65, 2463), (322, 1481, 260), (1409, 1415, 68)])
+def test_fp32_tiles_captured_and_on_two_streams(gpu_lib, M, N, K):
+    one, two = make(M, N, K, F, F, True, pads=(3, 3, 0, 0), seed=18), make(M, N, K, F, F, True, pads=(4, 4, 0, 0), seed=19)
+    torch.cuda.synchronize()
+    a, c = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(5):
+        call(*one, F, F, 2, 0, st=a.cuda_stream)
+        call(*two, F, F, 3, 1, st=c.cuda_stream)
+    torch.cuda.synchronize()
+    check(*one, F, 2, 0)
+    check(*two, F, 3, 1)
+    g, s = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(g, stream=s):
+        call(*one, F, F, 2, 0, st=s.cuda_stream)
+        call(*two, F, F, 3, 1, st=s.cuda_stream)
+    for i in range(3):
+        want = []
+        for t, act, first in ((one, 2, 0), (two, 3, 1)):
+            t[0].view.copy_(t[0].view.roll(1, 1))
+            call(*t, F, F, act, first)
+            want.append(t[4].view.clone())
+            t[4].view.fill_(MARK)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(one[4].view, want[0]) and torch.equal(two[4].view, want[1]), i
